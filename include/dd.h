@@ -73,6 +73,8 @@ typedef enum { DD_NORM_LAYER = 0, DD_NORM_RMS = 1 } dd_norm;
 #define DD_DEVERR_LOGITS 4 /* a row's logits gave no valid draw (NaN or +inf, or no finite
                               logit where one is needed); that row's output is a fallback:
                               z_s = z_t (posterior), z = 0 (verification) */
+#define DD_DEVERR_CACHE 8  /* cached context: a length, a block number or a row map does not fit (see
+                              dd_cache_plan, dd_cache_append, dd_cache_attention) */
 
 /*
  * Denoiser architecture.  Pre-LN transformer, bidirectional attention (other
@@ -480,6 +482,162 @@ dd_status dd_gaussian_latent_argmax(const int32_t* x, int32_t rows, int32_t V,
                                     uint32_t step, uint32_t row0, int32_t* z_out,
                                     int32_t* dev_err, void* stream);
 
+/* ---------------------------------------------------------------- cached context */
+
+/*
+ * A serving program keeps each request's context between passes instead of running it again: the keys
+ * and values of past positions stand in a cache in 8 bits, in blocks of `block` tokens that a pool
+ * hands out, and a pass runs on the new positions alone (the drafted block x_1 .. x_{B-1} and the
+ * token before it, Alg. 1; a prompt; the noisy block that is being decoded).
+ *
+ * Cache of one layer, with P = block, dh = head_dim (both buffers are the caller's):
+ *   codes   uint8 [n_blocks][n_kv_heads][2 P dh]: e4m3 numbers (OCP, 4 exponent and 3 mantissa bits,
+ *           largest 448, no infinities, NaN 0x7F / 0xFF); per block and head the keys [P][dh], then the
+ *           values [P / 32][dh][32] with tokens innermost (a lane of the attention's P V product reads
+ *           16 tokens of one feature at once).  16-byte aligned.
+ *   scales  fp32 [n_blocks][n_kv_heads][2]: the power of two 2^e, -100 <= e <= 120, by which the
+ *           block's key codes and its value codes are multiplied.  8-byte aligned.
+ * Powers of two keep a code's value exact when its block's scale changes (up to the codes' subnormals).
+ */
+typedef struct {
+    int32_t n_blocks;    /* blocks of the pool, >= 1; n_blocks * block < 2^31 */
+    int32_t block;       /* P: tokens per block: 32, 64, 128 or 256 */
+    int32_t n_kv_heads;  /* heads of keys and values, >= 1 */
+    int32_t head_dim;    /* dh: 32, 64 or 128 */
+} dd_cache;
+
+/*
+ * Which tokens a pass runs on and where they stand in the cache: device arrays of the caller's, written
+ * by dd_cache_plan and read by the other calls.  Rows are the pass's new tokens, T in the caller's
+ * buffers; sequence s owns rows row_start[s] .. row_start[s + 1] - 1, and rows from row_start[S] on are
+ * padding: nothing reads them and outputs leave them as they were.
+ */
+typedef struct {
+    int32_t S;             /* sequences, >= 0 */
+    int32_t T;             /* rows of the pass's buffers, >= 0 */
+    int32_t ld_table;      /* entries per row of block_table, >= 1 */
+    int32_t* block_table;  /* [S][ld_table]: block that holds tokens P j .. P j + P - 1 of sequence s */
+    int32_t* held;         /* [S]: blocks that sequence s holds (the table's first `held` entries) */
+    int32_t* kv_len;       /* [S]: tokens of sequence s with this pass's included */
+    int32_t* row_start;    /* [S + 1] */
+    int32_t* row_seq;      /* [T]: sequence of each row, -1 for padding */
+    int32_t* row_pos;      /* [T]: position of each row in its sequence, -1 for padding */
+    int32_t* slots;        /* [T]: block * P + place in the block of each row, -1 for padding */
+} dd_cache_map;
+
+/*
+ * dd_cache_plan - block tables and row maps of one pass from the requests' lengths, on the GPU (no
+ * length comes to the host).
+ *   seq_len      [S] tokens that sequence s has in the cache and keeps (after a verification: those before
+ *                the pass plus those accepted; what stands behind them is written over)
+ *   n_new        [S] tokens it adds in this pass, >= 0; -1 ends the sequence and gives its blocks back
+ *   held         [S] blocks it holds now; may be map->held itself
+ *   free_blocks  [n_blocks] a stack: its first *n_free entries are the blocks nobody holds.  Ended
+ *                sequences' blocks are pushed first, in the order of sequences and table entries, then
+ *                each sequence in order takes what it lacks from the top: ceil((seq_len + n_new) / P)
+ *                blocks less those it holds, written behind those in its table row
+ *   n_free_out   [1] the count afterwards; may be n_free itself
+ *   map          all its arrays are written, block_table only where a block is taken (an ended sequence
+ *                keeps its row, with held 0 and kv_len 0); map->kv_len may be seq_len itself.  The next
+ *                pass's seq_len is at most kv_len.
+ *   dev_err      NULL or device int32 error word
+ * The call does all of this or, where something does not fit, nothing: then DD_DEVERR_CACHE is set, no
+ * block changes hands, held, kv_len and n_free_out take held, seq_len and *n_free, and every row is
+ * padding.  That is so where the pool has too few blocks, the new tokens are more than T, a sequence
+ * would pass ld_table * P tokens, or an input is no plan's (a negative length, n_new below -1, seq_len
+ * beyond held * P, *n_free outside [0, n_blocks], more blocks given back than the stack has room for).
+ * A block number outside [0, n_blocks) in a table row that gets new tokens or in the stack sets
+ * DD_DEVERR_CACHE; the rows concerned get slot -1.
+ */
+dd_status dd_cache_plan(const dd_cache* cache, const dd_cache_map* map, const int32_t* seq_len,
+                        const int32_t* n_new, const int32_t* held, int32_t* free_blocks,
+                        const int32_t* n_free, int32_t* n_free_out, int32_t* dev_err, void* stream);
+
+/*
+ * dd_cache_append - keys and values of a pass's rows into the cache.
+ *   k, v         device [T] rows of n_kv_heads * dh numbers of `dtype`, head h at h * dh, row stride ld
+ *                elements (the packed q | k | v rows of a projection are read in place); 16-byte aligned,
+ *                ld * element size a multiple of 16, ld >= n_kv_heads * dh
+ *   Per block, head and kind (key or value), a the largest finite |x| of the rows that fall into it: the
+ *   scale is the smallest 2^e with a <= 448 * 2^e, e clamped to [-100, 120].  A block whose first new token
+ *   is not its first place has older tokens: it keeps its scale where that is larger, else takes the new
+ *   one and all its other codes are rounded again.  A code is x / 2^e rounded to nearest even; an
+ *   infinite or NaN x becomes a NaN code.
+ *   A row whose slot or sequence is out of range is left out and sets DD_DEVERR_CACHE.
+ * A sequence's rows are consecutive tokens (as dd_cache_plan lays them out), and no block belongs to two
+ * sequences.
+ */
+dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, const dd_cache_map* map,
+                          const void* k, const void* v, int32_t dtype, int64_t ld, int32_t* dev_err,
+                          void* stream);
+
+/*
+ * dd_cache_attention - attention of a pass's rows over their sequences' cached tokens, the pass's own
+ * among them (append first).
+ *   q            device [T] rows of n_heads * dh numbers of `dtype`, row stride ldq; query head h reads key
+ *                head h / (n_heads / n_kv_heads)
+ *   out          device [T] rows as q, row stride ldo: softmax(softmax_scale q k^T) v over the visible
+ *                tokens; zeros where a row sees none; padding rows are not written.  May not overlap q.
+ *   pattern      DD_ATTN_CAUSAL: row i of a sequence, at position kv_len - rows + i, sees the tokens up to
+ *                its own; DD_ATTN_BIDIRECTIONAL: every token of its sequence (a block that sees itself
+ *                whole).  Others: DD_E_UNSUPPORTED.
+ *   softmax_scale  in [1e-30, 1e30] (1 / sqrt(dh) is usual)
+ *   max_new, max_kv  bounds on a sequence's rows and on kv_len, 1 <= max_new, 1 <= max_kv <= ld_table * P;
+ *                they size the grid.  A sequence beyond them sets DD_DEVERR_CACHE: its rows past max_new
+ *                are not written, its tokens past max_kv are not seen.
+ *   ws           >= dd_cache_attention_workspace_bytes, 256-byte aligned (partial results of long caches;
+ *                NULL where that is 0); shared by no two calls that can overlap
+ * q and out are 16-byte aligned with row strides of a multiple of 16 bytes.  n_heads % n_kv_heads == 0.
+ * A table entry outside [0, n_blocks) sets DD_DEVERR_CACHE and its tokens are not seen.  A NaN in a
+ * key or value reaches the rows that see its token and no others.
+ * Arithmetic: products of exact e4m3 values with q in bf16 (fp32 q as the sum of three bf16 numbers),
+ * fp32 sums and softmax; the probabilities enter the product with v as q does (rounded to bf16, or the
+ * sum of three).
+ */
+size_t dd_cache_attention_workspace_bytes(const dd_cache* cache, int32_t S, int32_t T, int32_t n_heads,
+                                          int32_t max_new, int32_t max_kv);
+dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const float* scales,
+                             const dd_cache_map* map, const void* q, int64_t ldq, void* out, int64_t ldo,
+                             int32_t dtype, int32_t n_heads, int32_t pattern, double softmax_scale,
+                             int32_t max_new, int32_t max_kv, void* ws, size_t ws_bytes, int32_t* dev_err,
+                             void* stream);
+
+/*
+ * dd_logits_edit - penalties, biases and allowed tokens on rows of logits, before dd_posterior_sample or
+ * dd_spec_verify (edit p and q alike, and the verified tokens follow the edited target).
+ *   logits, out  device [rows][ld] of logits_dtype; out may be logits itself, or must not overlap it; columns
+ *                >= V are left untouched; ld >= V, ld % 8 == 0, 16-byte aligned
+ *   Row m belongs to sequence m / rows_per_seq; n_seq = ceil(rows / rows_per_seq).  For class v of row m:
+ *     c = how often v stands among the first hist_len[m] entries of the sequence's history
+ *     l' = (l > 0 ? l / repetition : l * repetition) - (presence + c frequency)   if c > 0, else l
+ *     l' = l' + the bias of v, if it has one
+ *     l' = -inf if the row's mask does not allow v
+ *   in fp32, rounded once to logits_dtype.
+ */
+typedef struct {
+    const int32_t* history;     /* [n_seq][ld_history] token ids; ids outside [0, V) (the mask, padding) are not
+                                   counted; NULL: no history */
+    int64_t ld_history;         /* entries per row, >= 0 */
+    const int32_t* hist_len;    /* [rows] entries that count, at most ld_history (more: all of them); negative:
+                                   the row passes unedited.  NULL: all of them */
+    const float* repetition;    /* [n_seq], > 0; NULL: 1 */
+    const float* presence;      /* [n_seq]; NULL: 0 */
+    const float* frequency;     /* [n_seq]; NULL: 0 */
+    const int32_t* bias_ids;    /* [n_seq][n_bias], ids outside [0, V) are skipped; an id listed twice takes its
+                                   last value; NULL: none */
+    const float* bias_values;   /* [n_seq][n_bias] */
+    int32_t n_bias;             /* >= 0 */
+    const uint32_t* allow;      /* [n_allow][ld_allow] bit masks, bit v % 32 of word v / 32 set where v is
+                                   allowed; NULL: everything is */
+    int64_t ld_allow;           /* words per mask, >= ceil(V / 32) */
+    int32_t n_allow;
+    const int32_t* allow_id;    /* [rows] mask of each row, -1: everything is allowed; other values outside
+                                   [0, n_allow) set DD_DEVERR_MASK and count as -1; NULL: mask 0 for all */
+} dd_logits_edits;
+dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V,
+                         void* out, int32_t rows_per_seq, const dd_logits_edits* edits, int32_t* dev_err,
+                         void* stream);
+
 /* ---------------------------------------------------------------- profiling */
 
 /*
@@ -492,7 +650,8 @@ dd_status dd_gaussian_latent_argmax(const int32_t* x, int32_t rows, int32_t V,
  * while it is off (the default) no launch touches it.
  * Classes: 0 time_embedding, 1 embed_layernorm, 2 layernorm, 3 gemm_qkv,
  * 4 attention, 5 gemm_attn_out, 6 gemm_mlp_up, 7 gemm_mlp_down, 8 gemm_vocab,
- * 9 posterior_sample, 10 gaussian_latent, 11 init_params, 12 copy, 13 compact_masked.
+ * 9 posterior_sample, 10 gaussian_latent, 11 init_params, 12 copy, 13 compact_masked,
+ * 14 gemm_lora_down, 15 cache_plan, 16 cache_append, 17 cache_attention, 18 logits_edit.
  */
 dd_status dd_profile_begin(int32_t max_launches, uint32_t class_mask);
 dd_status dd_profile_end(void);

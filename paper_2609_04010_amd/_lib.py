@@ -23,6 +23,7 @@ DD_GUMBEL_GROUP = 256
 DD_DEVERR_TOKEN = 1
 DD_DEVERR_MASK = 2
 DD_DEVERR_LOGITS = 4
+DD_DEVERR_CACHE = 8
 DD_LOOP_POSTERIOR_PASS = 1
 DD_LOOP_STORE_FREE = 2
 ATTN_PATTERNS = {"bidirectional": 0, "causal": 1, "block_causal": 2, "draft_train": 3}
@@ -37,7 +38,8 @@ EXPORTED = [
     "dd_attn_mask_build", "dd_denoise_forward_ex",
     "dd_posterior_sample", "dd_psi_posterior_sample", "dd_sample_loop", "dd_psi_sample_loop",
     "dd_gaussian_latent_argmax", "dd_spec_verify_workspace_bytes", "dd_spec_verify_noise_width",
-    "dd_spec_verify", "dd_spec_verify_noalloc", "dd_profile_begin",
+    "dd_spec_verify", "dd_spec_verify_noalloc", "dd_cache_plan", "dd_cache_append",
+    "dd_cache_attention_workspace_bytes", "dd_cache_attention", "dd_logits_edit", "dd_profile_begin",
     "dd_profile_end", "dd_profile_num_classes", "dd_profile_read",
 ]
 
@@ -58,6 +60,26 @@ class DDLoopWsLayout(ctypes.Structure):
                 ("logits_ld", ctypes.c_int64), ("glse_ld", ctypes.c_int64)]
 
 
+class DDCache(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int32), ("block", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class DDCacheMap(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int32), ("T", ctypes.c_int32), ("ld_table", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("row_start", ctypes.c_void_p), ("row_seq", ctypes.c_void_p), ("row_pos", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p)]
+
+
+class DDLogitsEdits(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("ld_history", ctypes.c_int64), ("hist_len", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
+                ("allow", ctypes.c_void_p), ("ld_allow", ctypes.c_int64), ("n_allow", ctypes.c_int32),
+                ("allow_id", ctypes.c_void_p)]
+
+
 class DDError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -76,6 +98,7 @@ def lib():
         c = ctypes
         P = c.c_void_p
         cfgp = c.POINTER(DDConfig)
+        cachep, mapp = c.POINTER(DDCache), c.POINTER(DDCacheMap)
         sig = {
             "dd_param_count": (c.c_int32, [cfgp]),
             "dd_param_tensor": (c.c_int32, [cfgp, c.c_int32, c.POINTER(c.c_size_t),
@@ -119,6 +142,14 @@ def lib():
                                            P]),
             "dd_spec_verify_noalloc": (c.c_int32, [P, P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, c.c_int32,
                                                    P, P, c.c_uint64, c.c_uint32, c.c_uint32, P, P, P, P]),
+            "dd_cache_plan": (c.c_int32, [cachep, mapp, P, P, P, P, P, P, P, P]),
+            "dd_cache_append": (c.c_int32, [cachep, P, P, mapp, P, P, c.c_int32, c.c_int64, P, P]),
+            "dd_cache_attention_workspace_bytes": (c.c_size_t, [cachep, c.c_int32, c.c_int32, c.c_int32, c.c_int32,
+                                                                c.c_int32]),
+            "dd_cache_attention": (c.c_int32, [cachep, P, P, mapp, P, c.c_int64, P, c.c_int64, c.c_int32, c.c_int32,
+                                               c.c_int32, c.c_double, c.c_int32, c.c_int32, P, c.c_size_t, P, P]),
+            "dd_logits_edit": (c.c_int32, [P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, P, c.c_int32,
+                                           c.POINTER(DDLogitsEdits), P, P]),
             "dd_profile_begin": (c.c_int32, [c.c_int32, c.c_uint32]),
             "dd_profile_end": (c.c_int32, []),
             "dd_profile_num_classes": (c.c_int32, []),
@@ -427,6 +458,177 @@ def gaussian_latent_argmax(x, rows, V, alpha_tilde, sigma, seed, step, z_out, ro
         _ptr(dev_err, 4, "dev_err", torch.int32) if dev_err is not None else None, _stream()))
 
 
+# ---------------------------------------------------------------- cached context
+
+def _here(device, name):
+    """The library runs on the current device: a tensor of another one is refused."""
+    if device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU, got {device}")
+    if device.index != _torch().cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU (cuda:{_torch().cuda.current_device()}), got {device}")
+
+
+def _dev(t, n, name, dtype):
+    """Device pointer of a contiguous tensor of at least n entries of `dtype` on the current GPU (0 for None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    _here(t.device, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < n:
+        raise ValueError(f"{name} holds {t.numel()} entries, needs {n}")
+    return t.data_ptr()
+
+
+def _rows(t, n, width, name, dtype=None):
+    """(device pointer, row stride) of a tensor [n or more][width or more] with neighbouring columns: a view of
+    columns of wider rows will do."""
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [{n}, {width}] with neighbouring columns, got {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    _here(t.device, name)
+    if t.shape[0] > 1 and t.stride(0) < width:
+        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)} for {width} columns)")
+    ld = t.stride(0)
+    if t.shape[0] <= 1:      # the stride of a single row says nothing
+        unit = 16 // t.element_size()
+        ld = (width + unit - 1) // unit * unit
+    return t.data_ptr(), ld
+
+
+def _float_code(t, name):
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
+        return DD_BF16
+    if t.dtype is torch.float32:
+        return DD_FP32
+    raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+
+
+def cache_config(n_blocks, block, n_kv_heads, head_dim):
+    """dd_cache of a pool: n_blocks blocks of `block` tokens, n_kv_heads heads of head_dim numbers."""
+    return DDCache(int(n_blocks), int(block), int(n_kv_heads), int(head_dim))
+
+
+def cache_tensors(cc, device="cuda"):
+    """(codes, scales) of one layer: uint8 [n_blocks, heads, 2 block dh] and fp32 [n_blocks, heads, 2], zeroed."""
+    torch = _torch()
+    return (torch.zeros((cc.n_blocks, cc.n_kv_heads, 2 * cc.block * cc.head_dim), dtype=torch.uint8, device=device),
+            torch.zeros((cc.n_blocks, cc.n_kv_heads, 2), dtype=torch.float32, device=device))
+
+
+class CacheMap:
+    """dd_cache_map over int32 tensors block_table [S, ld_table], held [S], kv_len [S], row_start [S + 1],
+    row_seq, row_pos and slots [T], which it keeps."""
+
+    def __init__(self, block_table, held, kv_len, row_start, row_seq, row_pos, slots):
+        i32 = _torch().int32
+        if block_table.dim() != 2:
+            raise ValueError("block_table must be [S, ld_table]")
+        S, ld = block_table.shape
+        T = row_seq.numel()
+        self.block_table, self.held, self.kv_len, self.row_start = block_table, held, kv_len, row_start
+        self.row_seq, self.row_pos, self.slots = row_seq, row_pos, slots
+        self.S, self.T, self.ld_table = S, T, ld
+        self.device = block_table.device
+        self.struct = DDCacheMap(S, T, ld, _dev(block_table, S * ld, "block_table", i32), _dev(held, S, "held", i32),
+                                 _dev(kv_len, S, "kv_len", i32), _dev(row_start, S + 1, "row_start", i32),
+                                 _dev(row_seq, T, "row_seq", i32), _dev(row_pos, T, "row_pos", i32),
+                                 _dev(slots, T, "slots", i32))
+
+    @classmethod
+    def empty(cls, S, T, ld_table, device="cuda"):
+        """A map of S sequences, T rows and tables of ld_table entries that hold no block yet."""
+        torch = _torch()
+        z = lambda *n: torch.zeros(n, dtype=torch.int32, device=device)   # noqa: E731
+        return cls(z(S, ld_table).fill_(-1), z(S), z(S), z(S + 1), z(T), z(T), z(T))
+
+
+def cache_plan(cc, m, seq_len, n_new, held, free_blocks, n_free, n_free_out, dev_err=None):
+    i32 = _torch().int32
+    _here(m.device, "map")
+    _check(lib().dd_cache_plan(
+        ctypes.byref(cc), ctypes.byref(m.struct), _dev(seq_len, m.S, "seq_len", i32), _dev(n_new, m.S, "n_new", i32),
+        _dev(held, m.S, "held", i32), _dev(free_blocks, cc.n_blocks, "free_blocks", i32), _dev(n_free, 1, "n_free", i32),
+        _dev(n_free_out, 1, "n_free_out", i32), _dev(dev_err, 1, "dev_err", i32), _stream()))
+
+
+def _cache_ptrs(cc, codes, scales):
+    torch = _torch()
+    n = cc.n_blocks * cc.n_kv_heads * 2
+    if codes.dtype is torch.float8_e4m3fn:
+        codes = codes.view(torch.uint8)
+    return (_dev(codes, n * cc.block * cc.head_dim, "codes", torch.uint8), _dev(scales, n, "scales", torch.float32))
+
+
+def cache_append(cc, codes, scales, m, k, v, dev_err=None):
+    """dd_cache_append; k and v are [T, n_kv_heads head_dim], of one type and row stride (views of packed rows)."""
+    _here(m.device, "map")
+    w = cc.n_kv_heads * cc.head_dim
+    code = _float_code(k, "k")
+    pk, ld = _rows(k, m.T, w, "k")
+    pv, ldv = _rows(v, m.T, w, "v", k.dtype)
+    if ld != ldv:
+        raise ValueError(f"k and v must have one row stride, got {ld} and {ldv}")
+    pc, ps = _cache_ptrs(cc, codes, scales)
+    _check(lib().dd_cache_append(ctypes.byref(cc), pc, ps, ctypes.byref(m.struct), pk, pv, code, ld,
+                                 _dev(dev_err, 1, "dev_err", _torch().int32), _stream()))
+
+
+def cache_attention_workspace_bytes(cc, S, T, n_heads, max_new, max_kv):
+    return int(lib().dd_cache_attention_workspace_bytes(ctypes.byref(cc), int(S), int(T), int(n_heads), int(max_new),
+                                                        int(max_kv)))
+
+
+def cache_attention(cc, codes, scales, m, q, out, n_heads, max_new, max_kv, ws=None, pattern="causal",
+                    softmax_scale=None, dev_err=None):
+    """dd_cache_attention; q and out are [T, n_heads head_dim]; softmax_scale defaults to head_dim ** -0.5."""
+    _here(m.device, "map")
+    w = n_heads * cc.head_dim
+    code = _float_code(q, "q")
+    pq, ldq = _rows(q, m.T, w, "q")
+    po, ldo = _rows(out, m.T, w, "out", q.dtype)
+    pc, ps = _cache_ptrs(cc, codes, scales)
+    if ws is not None:
+        _here(ws.device, "ws")
+    _check(lib().dd_cache_attention(
+        ctypes.byref(cc), pc, ps, ctypes.byref(m.struct), pq, ldq, po, ldo, code, int(n_heads), ATTN_PATTERNS[pattern],
+        float(softmax_scale if softmax_scale is not None else cc.head_dim ** -0.5), int(max_new), int(max_kv),
+        _ptr(ws, 0, "ws"), ws.numel() * ws.element_size() if ws is not None else 0,
+        _dev(dev_err, 1, "dev_err", _torch().int32), _stream()))
+
+
+def logits_edit(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, history=None, hist_len=None, repetition=None,
+                presence=None, frequency=None, bias_ids=None, bias_values=None, allow=None, allow_id=None, dev_err=None):
+    """dd_logits_edit; history [n_seq, entries], bias_ids / bias_values [n_seq, n_bias] and allow [n_allow, words]
+    give their sizes by their shapes (int32, or int32 holding the masks' bits)."""
+    torch = _torch()
+    i32, f32 = torch.int32, torch.float32
+    t = torch.bfloat16 if logits_dtype == "bf16" else f32
+    n_seq = -(-rows // rows_per_seq) if rows_per_seq > 0 else 0
+    for name, x in (("history", history), ("bias_ids", bias_ids), ("bias_values", bias_values), ("allow", allow)):
+        if x is not None and x.dim() != 2:
+            raise ValueError(f"{name} must have two dimensions")
+    if bias_ids is not None and bias_values is not None and bias_ids.shape != bias_values.shape:
+        raise ValueError(f"bias_ids {tuple(bias_ids.shape)} and bias_values {tuple(bias_values.shape)} differ")
+    lh = history.shape[1] if history is not None else 0
+    nb = bias_ids.shape[1] if bias_ids is not None else 0
+    na, la = allow.shape if allow is not None else (0, 0)
+    e = DDLogitsEdits(
+        _dev(history, n_seq * lh, "history", i32), lh, _dev(hist_len, rows, "hist_len", i32),
+        _dev(repetition, n_seq, "repetition", f32), _dev(presence, n_seq, "presence", f32),
+        _dev(frequency, n_seq, "frequency", f32), _dev(bias_ids, n_seq * nb, "bias_ids", i32),
+        _dev(bias_values, n_seq * nb, "bias_values", f32), nb, _dev(allow, na * la, "allow", i32), la, na,
+        _dev(allow_id, rows, "allow_id", i32))
+    _check(lib().dd_logits_edit(
+        _dev(logits, rows * ld, "logits", t), dtype_code(logits_dtype), int(ld), int(rows), int(V),
+        _dev(out, rows * ld, "out", t), int(rows_per_seq), ctypes.byref(e), _dev(dev_err, 1, "dev_err", i32), _stream()))
+
+
 def workspace_reset(ws):
     _check(lib().dd_workspace_reset(_ptr(ws, 4, "ws"), _stream()))
 
@@ -442,7 +644,7 @@ def read_device_error(err):
 PROFILE_CLASSES = ["time_embedding", "embed_layernorm", "layernorm", "gemm_qkv", "attention",
                    "gemm_attn_out", "gemm_mlp_up", "gemm_mlp_down", "gemm_vocab",
                    "posterior_sample", "gaussian_latent", "init_params", "copy", "compact_masked",
-                   "gemm_lora_down"]
+                   "gemm_lora_down", "cache_plan", "cache_append", "cache_attention", "logits_edit"]
 
 
 def profile_begin(max_launches, classes=None):

@@ -16,12 +16,12 @@ LIB = os.path.join(PKG, "libdd.so")
 
 SOURCES = ["dd_api.hip", "k_posterior.hip", "k_latent_init.hip", "k_norm.hip", "k_gemm.hip",
            "k_gemm_ring.hip",
-           "k_attn.hip", "k_verify.hip"]
+           "k_attn.hip", "k_verify.hip", "k_cache.hip", "k_cache_attn.hip", "k_edit.hip"]
 
 # Per-file extra flags.  Attention keeps its MFMA accumulators in ordinary VGPRs (the softmax reads
 # every score with VALU instructions; AGPR accumulators would need a copy per score).  The GEMMs need
 # the AGPR file for their 256 accumulators and keep the default.
-EXTRA = {"k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("k_attn.hip", "k_cache_attn.hip")}
 
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
          # packed-FP32 instructions stay off everywhere: some of their forms have given wrong results

@@ -92,6 +92,7 @@ dd_status launch_status(const char* what);
 enum KernelClass {
     KC_TEMB = 0, KC_EMBED_LN, KC_LN, KC_GEMM_QKV, KC_ATTN, KC_GEMM_O, KC_GEMM_MLP1,
     KC_GEMM_MLP2, KC_GEMM_VOCAB, KC_POSTERIOR, KC_LATENT, KC_INIT, KC_COPY, KC_COMPACT, KC_GEMM_LORA,
+    KC_CACHE_PLAN, KC_CACHE_APPEND, KC_CACHE_ATTN, KC_LOGITS_EDIT,
     KC_COUNT
 };
 // A scope around one kernel launch (kernel = true) hands its event pair to that launch (launch_k),

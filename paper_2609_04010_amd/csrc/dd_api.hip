@@ -13,6 +13,7 @@
 #include <mutex>
 #include <vector>
 
+#include "cache.h"
 #include "kernels.h"
 
 namespace dd {
@@ -54,7 +55,8 @@ dd_status launch_status(const char* what) {
 static const char* kClassNames[KC_COUNT] = {
     "time_embedding", "embed_layernorm", "layernorm", "gemm_qkv", "attention", "gemm_attn_out",
     "gemm_mlp_up", "gemm_mlp_down", "gemm_vocab", "posterior_sample", "gaussian_latent",
-    "init_params", "copy", "compact_masked", "gemm_lora_down"};
+    "init_params", "copy", "compact_masked", "gemm_lora_down", "cache_plan",
+    "cache_append", "cache_attention", "logits_edit"};
 
 // The recorder is the library's only process-wide mutable state: guarded by g_prof_mu, and skipped
 // without taking the lock while it is off.
@@ -867,6 +869,133 @@ dd_status dd_gaussian_latent_argmax(const int32_t* x, int32_t rows, int32_t V, d
     DD_CHECK(x && z_out, DD_E_ARG, "NULL pointer argument");
     return launch_latent(x, rows, V, alpha_tilde, sigma, seed, step, row0, z_out, dev_err,
                          (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- cached context
+
+static dd_status cache_check(const dd_cache* c) {
+    DD_CHECK(c, DD_E_ARG, "cache is NULL");
+    DD_CHECK(c->n_blocks > 0 && c->n_kv_heads > 0, DD_E_ARG, "n_blocks and n_kv_heads must be positive");
+    DD_CHECK(c->block == 32 || c->block == 64 || c->block == 128 || c->block == 256, DD_E_UNSUPPORTED,
+             "cache blocks hold 32, 64, 128 or 256 tokens (got %d)", c->block);
+    DD_CHECK(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128, DD_E_UNSUPPORTED,
+             "head dim %d unsupported by the cache (32, 64 or 128)", c->head_dim);
+    DD_CHECK((int64_t)c->n_blocks * c->block <= INT32_MAX, DD_E_UNSUPPORTED, "n_blocks * block must be below 2^31");
+    DD_CHECK(c->n_kv_heads <= 16384, DD_E_UNSUPPORTED, "more than 16384 key heads unsupported");
+    return DD_OK;
+}
+
+static dd_status map_check(const dd_cache_map* m) {
+    DD_CHECK(m, DD_E_ARG, "map is NULL");
+    DD_CHECK(m->S >= 0 && m->T >= 0 && m->ld_table >= 1, DD_E_ARG, "map sizes must not be negative, ld_table positive");
+    DD_CHECK(m->row_start, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(m->S == 0 || (m->block_table && m->held && m->kv_len), DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(m->T == 0 || (m->row_seq && m->row_pos && m->slots), DD_E_ARG, "NULL pointer argument");
+    return DD_OK;
+}
+
+dd_status dd_cache_plan(const dd_cache* cache, const dd_cache_map* map, const int32_t* seq_len, const int32_t* n_new,
+                        const int32_t* held, int32_t* free_blocks, const int32_t* n_free, int32_t* n_free_out,
+                        int32_t* dev_err, void* stream) {
+    DD_TRY(cache_check(cache));
+    DD_TRY(map_check(map));
+    DD_CHECK(map->S == 0 || (seq_len && n_new && held), DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(free_blocks && n_free && n_free_out, DD_E_ARG, "NULL pointer argument");
+    PlanArgs a = {cache_shape(cache), map->S, map->T, map->ld_table, map->block_table, map->held, map->kv_len,
+                  map->row_start, map->row_seq, map->row_pos, map->slots, seq_len, n_new, held, free_blocks, n_free,
+                  n_free_out, dev_err};
+    return launch_cache_plan(a, (hipStream_t)stream);
+}
+
+dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, const dd_cache_map* map, const void* k,
+                          const void* v, int32_t dtype, int64_t ld, int32_t* dev_err, void* stream) {
+    DD_TRY(cache_check(cache));
+    DD_TRY(map_check(map));
+    DD_CHECK(dtype == DD_BF16 || dtype == DD_FP32, DD_E_DTYPE, "unknown dtype");
+    DD_CHECK(ld >= (int64_t)cache->n_kv_heads * cache->head_dim && ld * (int64_t)esize(dtype) % 16 == 0, DD_E_SHAPE,
+             "ld must be >= n_kv_heads * head_dim and a multiple of 16 bytes");
+    if (map->S == 0 || map->T == 0) return DD_OK;
+    DD_CHECK(codes && scales && k && v, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK((((uintptr_t)codes | (uintptr_t)k | (uintptr_t)v) & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
+             "codes, k and v must be 16-byte aligned, scales 8-byte aligned");
+    AppendArgs a = {cache_shape(cache), cache->head_dim, map->S, map->T, (uint8_t*)codes, scales, map->row_start,
+                    map->row_seq, map->slots, k, v, ld, 0, dev_err};
+    return launch_cache_append(dtype, a, (hipStream_t)stream);
+}
+
+// Shape checks shared by dd_cache_attention and its workspace query.
+static dd_status cache_attn_check(const dd_cache* cache, int32_t S, int32_t T, int32_t n_heads, int32_t max_new,
+                                  int32_t max_kv) {
+    DD_TRY(cache_check(cache));
+    DD_CHECK(S >= 0 && T >= 0 && n_heads > 0 && max_new > 0 && max_kv > 0, DD_E_ARG,
+             "n_heads, max_new and max_kv must be positive");
+    DD_CHECK(n_heads % cache->n_kv_heads == 0, DD_E_SHAPE, "n_heads must be a multiple of n_kv_heads");
+    DD_CHECK((int64_t)max_kv <= INT32_MAX - 256 && (int64_t)max_new * n_heads <= INT32_MAX - 256, DD_E_UNSUPPORTED,
+             "max_kv or max_new * n_heads too large");
+    if (S == 0 || T == 0) return DD_OK;
+    const CacheAttnPlan p = cache_attn_plan(S, T, cache->n_kv_heads, n_heads, cache->head_dim, max_new, max_kv);
+    const int64_t tiles = ceil_div((int64_t)max_new * (n_heads / cache->n_kv_heads), 32 * (4 / p.kw));
+    const double wgs = ((double)S * cache->n_kv_heads * p.nsplit + 8) * (double)tiles;
+    DD_CHECK(wgs < 2147483647.0 && (double)S * max_new * n_heads < 2147483647.0, DD_E_UNSUPPORTED,
+             "too many workgroups: S * max_new * n_heads is too large");
+    return DD_OK;
+}
+
+size_t dd_cache_attention_workspace_bytes(const dd_cache* cache, int32_t S, int32_t T, int32_t n_heads, int32_t max_new,
+                                          int32_t max_kv) {
+    if (cache_attn_check(cache, S, T, n_heads, max_new, max_kv) != DD_OK || S == 0 || T == 0) return 0;
+    return cache_attn_plan(S, T, cache->n_kv_heads, n_heads, cache->head_dim, max_new, max_kv).ws;
+}
+
+dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const float* scales, const dd_cache_map* map,
+                             const void* q, int64_t ldq, void* out, int64_t ldo, int32_t dtype, int32_t n_heads,
+                             int32_t pattern, double softmax_scale, int32_t max_new, int32_t max_kv, void* ws,
+                             size_t ws_bytes, int32_t* dev_err, void* stream) {
+    DD_TRY(map_check(map));
+    DD_TRY(cache_attn_check(cache, map->S, map->T, n_heads, max_new, max_kv));
+    DD_CHECK(dtype == DD_BF16 || dtype == DD_FP32, DD_E_DTYPE, "unknown dtype");
+    DD_CHECK(pattern == DD_ATTN_CAUSAL || pattern == DD_ATTN_BIDIRECTIONAL, DD_E_UNSUPPORTED,
+             "attention over the cache is causal or bidirectional (got pattern %d)", pattern);
+    DD_CHECK(softmax_scale >= 1e-30 && softmax_scale <= 1e30, DD_E_ARG, "softmax_scale must lie in [1e-30, 1e30]");
+    DD_CHECK((int64_t)max_kv <= (int64_t)map->ld_table * cache->block, DD_E_SHAPE, "max_kv exceeds ld_table * block");
+    const int64_t w = (int64_t)n_heads * cache->head_dim, es = (int64_t)esize(dtype);
+    DD_CHECK(ldq >= w && ldo >= w && ldq * es % 16 == 0 && ldo * es % 16 == 0, DD_E_SHAPE,
+             "ldq and ldo must be >= n_heads * head_dim and multiples of 16 bytes");
+    if (map->S == 0 || map->T == 0) return DD_OK;
+    DD_CHECK(codes && scales && q && out, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK((((uintptr_t)codes | (uintptr_t)q | (uintptr_t)out) & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
+             "codes, q and out must be 16-byte aligned, scales 8-byte aligned");
+    const CacheAttnPlan p =
+        cache_attn_plan(map->S, map->T, cache->n_kv_heads, n_heads, cache->head_dim, max_new, max_kv);
+    DD_CHECK(p.ws == 0 || (ws && ((uintptr_t)ws & 255) == 0), DD_E_ARG, "ws must be a 256-byte aligned buffer");
+    DD_CHECK(ws_bytes >= p.ws, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, p.ws);
+    CacheAttnArgs a = {cache_shape(cache), cache->head_dim, map->S, map->T, map->ld_table, (const uint8_t*)codes, scales,
+                       map->block_table, map->kv_len, map->row_start, q, ldq, out, ldo, n_heads,
+                       n_heads / cache->n_kv_heads, pattern == DD_ATTN_CAUSAL,
+                       (float)(softmax_scale * 1.4426950408889634), max_new, max_kv, p.chunk, p.nsplit, (float*)ws,
+                       dev_err};
+    return launch_cache_attn(dtype, a, p.kw, (hipStream_t)stream);
+}
+
+dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V, void* out,
+                         int32_t rows_per_seq, const dd_logits_edits* edits, int32_t* dev_err, void* stream) {
+    DD_CHECK(logits_dtype == DD_BF16 || logits_dtype == DD_FP32, DD_E_DTYPE, "unknown logits dtype");
+    DD_CHECK(rows >= 0 && V > 0 && rows_per_seq > 0, DD_E_ARG, "rows must be >= 0, V and rows_per_seq > 0");
+    DD_CHECK(V <= (1 << 24), DD_E_UNSUPPORTED, "V > 2^24 unsupported");
+    DD_CHECK(ld >= V && ld % 8 == 0, DD_E_SHAPE, "ld must be >= V and a multiple of 8");
+    DD_CHECK(edits, DD_E_ARG, "edits is NULL");
+    DD_CHECK(edits->ld_history >= 0 && edits->ld_history <= INT32_MAX && edits->n_bias >= 0 && edits->n_allow >= 0, DD_E_ARG,
+             "history, bias and mask sizes must not be negative");
+    DD_CHECK(!edits->bias_ids == !edits->bias_values, DD_E_ARG, "bias_ids and bias_values go together");
+    DD_CHECK(edits->allow || !edits->allow_id, DD_E_ARG, "allow_id given without masks");
+    DD_CHECK(!edits->allow || (edits->n_allow > 0 && edits->ld_allow >= ((int64_t)V + 31) / 32), DD_E_SHAPE,
+             "masks need n_allow > 0 and ld_allow >= ceil(V / 32)");
+    if (rows == 0) return DD_OK;
+    DD_CHECK(logits && out, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK((((uintptr_t)logits | (uintptr_t)out) & 15) == 0, DD_E_ARG, "logits and out must be 16-byte aligned");
+    EditArgs a = {logits, out, ld, rows, V, rows_per_seq, *edits, 0, dev_err};
+    if (!a.e.history) a.e.ld_history = 0;
+    return launch_edit(a, logits_dtype, (hipStream_t)stream);
 }
 
 dd_status dd_profile_begin(int32_t max_launches, uint32_t class_mask) {
