@@ -603,6 +603,32 @@ dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const flo
                              void* stream);
 
 /*
+ * dd_denoise_forward_cached - the denoiser on a pass's rows over their sequences' cached context: as
+ * dd_denoise_forward_ex on the whole sequences under `pattern`, but for the rounding of keys and values to
+ * the cache's 8 bits, and with the new rows alone computed.  Every layer appends the rows' keys and values to
+ * its part of the cache and attends over it.
+ *   z_t          device int32 [T], the token of each row; padding rows' tokens are not looked at
+ *   alpha_t      conditions the time embedding (1 for a clean context and its verification)
+ *   cache        n_kv_heads = cfg->n_heads, head_dim = d_model / n_heads
+ *   codes, scales  the cache of every layer in turn: [n_layers] of what dd_cache describes
+ *   map          of dd_cache_plan, run before this call on the same stream; positions beyond max_len set
+ *                DD_DEVERR_CACHE
+ *   pattern      DD_ATTN_CAUSAL: the AR pathway, drafting and verification; DD_ATTN_BIDIRECTIONAL: a block that
+ *                sees its context and itself whole.  A context attends as it did in the pass that appended it.
+ *   max_new, max_kv  as in dd_cache_attention; max_kv <= max_len
+ *   lora_gate    NULL (all adapters on) or device int32 [T]: row r uses its adapters iff lora_gate[r] != 0
+ *   logits       device [T][ld]; padding rows hold nothing meaningful
+ *   ws           device workspace of >= dd_cached_workspace_bytes bytes (the device error word is its first int32)
+ * Alignment and errors as dd_denoise_forward.
+ */
+size_t dd_cached_workspace_bytes(const dd_config* cfg, const dd_cache* cache, int32_t S, int32_t T, int32_t max_new,
+                                 int32_t max_kv);
+dd_status dd_denoise_forward_cached(const dd_config* cfg, const void* params, const int32_t* z_t, double alpha_t,
+                                    const dd_cache* cache, void* codes, float* scales, const dd_cache_map* map,
+                                    int32_t pattern, int32_t max_new, int32_t max_kv, const int32_t* lora_gate,
+                                    void* logits, int64_t ld, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * dd_logits_edit - penalties, biases and allowed tokens on rows of logits, before dd_posterior_sample or
  * dd_spec_verify (edit p and q alike, and the verified tokens follow the edited target).
  *   logits, out  device [rows][ld] of logits_dtype; out may be logits itself, or must not overlap it; columns

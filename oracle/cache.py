@@ -201,3 +201,39 @@ def edit(l, seq, history=None, hist_len=None, repetition=None, presence=None, fr
             if 0 <= a < len(allow):
                 l[m, ~allow[a]] = -np.inf
     return l
+
+
+def forward_cached(cfg, P, z, alpha_t, codes, scales, block, table, kv_len, row_start, causal=True, gate=None):
+    """The denoiser on rows z [T] over caches that already hold the rows' own keys and values: codes uint8
+    [layers, n_blocks, H, 2 block dh], scales [layers, n_blocks, H, 2].  Returns the logits [T, V] (zero rows of
+    padding) and every layer's keys and values [T, H, dh] before their rounding."""
+    from . import forward as fw
+    T, d, H = len(z), cfg["d_model"], cfg["n_heads"]
+    dh, S = d // H, len(kv_len)
+    pos, live = np.zeros(T, int), np.zeros(T, bool)
+    for s in range(S):
+        n = row_start[s + 1] - row_start[s]
+        pos[row_start[s]:row_start[s + 1]] = kv_len[s] - n + np.arange(n)
+        live[row_start[s]:row_start[s + 1]] = True
+    g = np.ones(T) if gate is None else np.asarray(gate, dtype=np.float64)
+    h = P["tok_emb"][np.where(live, z, 0)] + P["pos_emb"][pos]
+    if cfg.get("time_cond", True):
+        h = h + fw.time_embedding(alpha_t, d)[None]
+    kvs = []
+    for l in range(cfg["n_layers"]):
+        p = lambda n: P[f"l{l}.{n}"]   # noqa: E731
+        proj = lambda name, a: fw.projection(cfg, P, l, name, a[None], g)[0]   # noqa: E731
+        qkv = proj("qkv", fw.normalise(cfg, h, p("ln1_g"), p("ln1_b"))).reshape(T, 3, H, dh)
+        kvs.append((qkv[:, 1], qkv[:, 2]))
+        o = np.zeros((T, H, dh))
+        for s in range(S):
+            r0, r1, L = row_start[s], row_start[s + 1], int(kv_len[s])
+            if r1 > r0:
+                k, v = gather(codes[l], scales[l], block, dh, table[s][:-(-L // block)], L)
+                o[r0:r1] = attention(qkv[r0:r1, 0], k, v, L - (r1 - r0), causal, dh ** -0.5)
+        h = h + proj("o", o.reshape(T, d))
+        a = fw.normalise(cfg, h, p("ln2_g"), p("ln2_b"))
+        h = h + proj("2", fw.gelu_tanh(proj("1", a)))
+    out = fw.normalise(cfg, h, P["lnf_g"], P["lnf_b"]) @ P["w_out"].T
+    out[~live] = 0
+    return out, kvs

@@ -39,7 +39,8 @@ EXPORTED = [
     "dd_posterior_sample", "dd_psi_posterior_sample", "dd_sample_loop", "dd_psi_sample_loop",
     "dd_gaussian_latent_argmax", "dd_spec_verify_workspace_bytes", "dd_spec_verify_noise_width",
     "dd_spec_verify", "dd_spec_verify_noalloc", "dd_cache_plan", "dd_cache_append",
-    "dd_cache_attention_workspace_bytes", "dd_cache_attention", "dd_logits_edit", "dd_profile_begin",
+    "dd_cache_attention_workspace_bytes", "dd_cache_attention", "dd_logits_edit", "dd_cached_workspace_bytes",
+    "dd_denoise_forward_cached", "dd_profile_begin",
     "dd_profile_end", "dd_profile_num_classes", "dd_profile_read",
 ]
 
@@ -148,6 +149,9 @@ def lib():
                                                                 c.c_int32]),
             "dd_cache_attention": (c.c_int32, [cachep, P, P, mapp, P, c.c_int64, P, c.c_int64, c.c_int32, c.c_int32,
                                                c.c_int32, c.c_double, c.c_int32, c.c_int32, P, c.c_size_t, P, P]),
+            "dd_cached_workspace_bytes": (c.c_size_t, [cfgp, cachep, c.c_int32, c.c_int32, c.c_int32, c.c_int32]),
+            "dd_denoise_forward_cached": (c.c_int32, [cfgp, P, P, c.c_double, cachep, P, P, mapp, c.c_int32, c.c_int32,
+                                                      c.c_int32, P, P, c.c_int64, P, c.c_size_t, P]),
             "dd_logits_edit": (c.c_int32, [P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, P, c.c_int32,
                                            c.POINTER(DDLogitsEdits), P, P]),
             "dd_profile_begin": (c.c_int32, [c.c_int32, c.c_uint32]),
@@ -514,11 +518,13 @@ def cache_config(n_blocks, block, n_kv_heads, head_dim):
     return DDCache(int(n_blocks), int(block), int(n_kv_heads), int(head_dim))
 
 
-def cache_tensors(cc, device="cuda"):
-    """(codes, scales) of one layer: uint8 [n_blocks, heads, 2 block dh] and fp32 [n_blocks, heads, 2], zeroed."""
+def cache_tensors(cc, layers=None, device="cuda"):
+    """(codes, scales) of one layer, uint8 [n_blocks, heads, 2 block dh] and fp32 [n_blocks, heads, 2], or of
+    `layers` of them in front; zeroed."""
     torch = _torch()
-    return (torch.zeros((cc.n_blocks, cc.n_kv_heads, 2 * cc.block * cc.head_dim), dtype=torch.uint8, device=device),
-            torch.zeros((cc.n_blocks, cc.n_kv_heads, 2), dtype=torch.float32, device=device))
+    lead = (cc.n_blocks, cc.n_kv_heads) if layers is None else (layers, cc.n_blocks, cc.n_kv_heads)
+    return (torch.zeros((*lead, 2 * cc.block * cc.head_dim), dtype=torch.uint8, device=device),
+            torch.zeros((*lead, 2), dtype=torch.float32, device=device))
 
 
 class CacheMap:
@@ -600,6 +606,30 @@ def cache_attention(cc, codes, scales, m, q, out, n_heads, max_new, max_kv, ws=N
         float(softmax_scale if softmax_scale is not None else cc.head_dim ** -0.5), int(max_new), int(max_kv),
         _ptr(ws, 0, "ws"), ws.numel() * ws.element_size() if ws is not None else 0,
         _dev(dev_err, 1, "dev_err", _torch().int32), _stream()))
+
+
+def cached_workspace_bytes(cfg, cc, S, T, max_new, max_kv):
+    return int(lib().dd_cached_workspace_bytes(ctypes.byref(make_config(cfg)), ctypes.byref(cc), int(S), int(T),
+                                               int(max_new), int(max_kv)))
+
+
+def denoise_forward_cached(cfg, params, z_t, alpha_t, cc, codes, scales, m, logits, ld, ws, max_new, max_kv,
+                           pattern="causal", lora_gate=None):
+    """dd_denoise_forward_cached; codes and scales hold the caches of the n_layers layers (cache_tensors with
+    layers=n_layers)."""
+    torch = _torch()
+    es = 2 if cfg["dtype"] == "bf16" else 4
+    i32 = torch.int32
+    _here(m.device, "map")
+    n = cfg["n_layers"] * cc.n_blocks * cc.n_kv_heads * 2
+    if codes.dtype is torch.float8_e4m3fn:
+        codes = codes.view(torch.uint8)
+    _check(lib().dd_denoise_forward_cached(
+        ctypes.byref(make_config(cfg)), _ptr(params, param_bytes(cfg), "params"), _dev(z_t, m.T, "z_t", i32), float(alpha_t),
+        ctypes.byref(cc), _dev(codes, n * cc.block * cc.head_dim, "codes", torch.uint8), _dev(scales, n, "scales", torch.float32),
+        ctypes.byref(m.struct), ATTN_PATTERNS[pattern], int(max_new), int(max_kv), _dev(lora_gate, m.T, "lora_gate", i32),
+        _ptr(logits, es * m.T * ld, "logits"), int(ld),
+        _ptr(ws, cached_workspace_bytes(cfg, cc, m.S, m.T, max_new, max_kv), "ws"), ws.numel() * ws.element_size(), _stream()))
 
 
 def logits_edit(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, history=None, hist_len=None, repetition=None,

@@ -248,6 +248,18 @@ static dd_status forward_check(const dd_config* c) {
     return DD_OK;
 }
 
+// A pass over a cached context: every layer's keys and values go into its part of the cache and its
+// attention runs over that.
+struct CachedPass {
+    const dd_cache* cache;
+    char* codes;             // [n_layers] of the cache's codes, then of its scales
+    float* scales;
+    const dd_cache_map* map;
+    int32_t pattern, max_new, max_kv;
+    void* ws;                // of dd_cache_attention
+    size_t ws_bytes;
+};
+
 // vocab_rows / vocab_count (device, nullable): restrict the vocabulary projection to the listed
 // rows, written compacted (row j of `logits` belongs to token row vocab_rows[j]).
 // attn_mask (device [3L], nullable): visibility pattern; lora_gate (device [L], nullable): adapter
@@ -261,7 +273,8 @@ static dd_status run_forward(const dd_config* c, const void* params, const int32
                              const int32_t* attn_mask = nullptr, const int32_t* lora_gate = nullptr,
                              float* vocab_lse = nullptr, int64_t lse_ld = 0,
                              int32_t* vocab_cand = nullptr, uint64_t cand_seed = 0,
-                             uint32_t cand_step = 0, const int32_t* vocab_seq = nullptr) {
+                             uint32_t cand_step = 0, const int32_t* vocab_seq = nullptr,
+                             const CachedPass* cached = nullptr) {
     const std::vector<Tensor> T = tensor_list(c);
     const WsLayout w = ws_layout(c, (int64_t)B * L);
     const char* P = (const char*)params;
@@ -320,8 +333,9 @@ static dd_status run_forward(const dd_config* c, const void* params, const int32
                            !attn_mask && gemm_gather_supported(dt, d) && gemm_gather_supported(dt, F);
     if (c->time_cond) DD_TRY(launch_temb(temb, d, 1000.0 * (1.0 - alpha_t), s));
     const int g0 = nl > 0 ? 2 : lnf;
-    DD_TRY(launch_embed_ln(dt, c->norm, z, M, L, n_tok(c), d, tp(0), tp(1), c->time_cond ? temb : nullptr,
-                           tp(g0), tp(g0 + 1), c->norm_eps, h, xln, dr, err, s));
+    DD_TRY(launch_embed_ln(dt, c->norm, z, M, cached ? c->max_len : L, n_tok(c), d, tp(0), tp(1),
+                           c->time_cond ? temb : nullptr, tp(g0), tp(g0 + 1), c->norm_eps, h, xln, dr, err, s,
+                           cached ? cached->map->row_pos : nullptr));
     for (int l = 0; l < nl; ++l) {
         const int b = 2 + 12 * l;
         const int a0 = lnf + 3 + 4 * l;   // this layer's A matrices (adapters only)
@@ -336,7 +350,20 @@ static dd_status run_forward(const dd_config* c, const void* params, const int32
             aa.qrows = vocab_rows;
             aa.qseq = vocab_seq;
         }
-        DD_TRY(launch_attn(dt, aa, s));
+        if (cached) {
+            const dd_cache* cc = cached->cache;
+            const int64_t unit = (int64_t)cc->n_blocks * cc->n_kv_heads * 2;
+            void* codes = cached->codes + l * unit * cc->block * cc->head_dim;
+            float* scales = cached->scales + l * unit;
+            const char* qp = (const char*)qkv;
+            DD_TRY(dd_cache_append(cc, codes, scales, cached->map, qp + (size_t)d * es, qp + (size_t)(2 * d) * es, dt,
+                                   3 * d, err, s));
+            DD_TRY(dd_cache_attention(cc, codes, scales, cached->map, qp, 3 * d, att, dr, dt, H, cached->pattern,
+                                      1.0 / sqrt((double)(d / H)), cached->max_new, cached->max_kv, cached->ws,
+                                      cached->ws_bytes, err, s));
+        } else {
+            DD_TRY(launch_attn(dt, aa, s));
+        }
         if (tail) {
             // The listed rows are few in most steps (about M / T from an all-mask start), where the
             // 256-row tiles leave most CUs idle through a whole K loop.  Up to TAIL_ROWS rows ring
@@ -410,7 +437,6 @@ static dd_status run_forward(const dd_config* c, const void* params, const int32
     g.step = cand_step;
     g.row0 = 0;
     DD_TRY(launch_gemm(dt, vocab_cand ? EPI_LSE_CDF : vocab_lse ? EPI_LSE : EPI_PLAIN, KC_GEMM_VOCAB, g, s));
-    (void)es;
     return DD_OK;
 }
 
@@ -975,6 +1001,50 @@ dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const flo
                        (float)(softmax_scale * 1.4426950408889634), max_new, max_kv, p.chunk, p.nsplit, (float*)ws,
                        dev_err};
     return launch_cache_attn(dtype, a, p.kw, (hipStream_t)stream);
+}
+
+// Checks of a pass over a cached context that need no buffers.
+static dd_status cached_check(const dd_config* cfg, const dd_cache* cache, int32_t S, int32_t T, int32_t max_new,
+                              int32_t max_kv) {
+    DD_TRY(cfg_check(cfg));
+    DD_TRY(forward_check(cfg));
+    DD_TRY(cache_attn_check(cache, S, T, cfg->n_heads, max_new, max_kv));
+    DD_CHECK(cache->n_kv_heads == cfg->n_heads && cache->head_dim == cfg->d_model / cfg->n_heads, DD_E_SHAPE,
+             "the cache holds %d heads of %d, the model has %d of %d", cache->n_kv_heads, cache->head_dim,
+             cfg->n_heads, cfg->d_model / cfg->n_heads);
+    DD_CHECK(max_kv <= cfg->max_len, DD_E_SHAPE, "max_kv = %d exceeds max_len = %d", max_kv, cfg->max_len);
+    return DD_OK;
+}
+
+size_t dd_cached_workspace_bytes(const dd_config* cfg, const dd_cache* cache, int32_t S, int32_t T, int32_t max_new,
+                                 int32_t max_kv) {
+    if (cached_check(cfg, cache, S, T, max_new, max_kv) != DD_OK || S == 0 || T == 0) return 0;
+    return ws_layout(cfg, T).total_fwd + dd_cache_attention_workspace_bytes(cache, S, T, cfg->n_heads, max_new, max_kv);
+}
+
+dd_status dd_denoise_forward_cached(const dd_config* cfg, const void* params, const int32_t* z_t, double alpha_t,
+                                    const dd_cache* cache, void* codes, float* scales, const dd_cache_map* map,
+                                    int32_t pattern, int32_t max_new, int32_t max_kv, const int32_t* lora_gate,
+                                    void* logits, int64_t ld, void* ws, size_t ws_bytes, void* stream) {
+    DD_TRY(map_check(map));
+    DD_TRY(cached_check(cfg, cache, map->S, map->T, max_new, max_kv));
+    DD_CHECK(!lora_gate || cfg->lora_rank > 0, DD_E_ARG, "lora_gate given for a model without adapters");
+    DD_CHECK(pattern == DD_ATTN_CAUSAL || pattern == DD_ATTN_BIDIRECTIONAL, DD_E_UNSUPPORTED,
+             "attention over the cache is causal or bidirectional (got pattern %d)", pattern);
+    DD_CHECK((int64_t)max_kv <= (int64_t)map->ld_table * cache->block, DD_E_SHAPE, "max_kv exceeds ld_table * block");
+    DD_CHECK(alpha_t >= 0.0 && alpha_t <= 1.0, DD_E_ARG, "alpha_t must lie in [0, 1]");
+    DD_CHECK(ld >= cfg->vocab && ld % 8 == 0, DD_E_SHAPE, "ld must be >= V and a multiple of 8");
+    if (map->S == 0 || map->T == 0) return DD_OK;
+    DD_CHECK(params && z_t && codes && scales && logits && ws, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK((((uintptr_t)logits | (uintptr_t)codes) & 15) == 0 && ((uintptr_t)scales & 7) == 0 &&
+                 ((uintptr_t)ws & 255) == 0 && ((uintptr_t)params & 255) == 0,
+             DD_E_ARG, "logits and codes must be 16-byte aligned, scales 8-byte, params and ws 256-byte aligned");
+    const size_t fwd = ws_layout(cfg, map->T).total_fwd;
+    const size_t need = dd_cached_workspace_bytes(cfg, cache, map->S, map->T, max_new, max_kv);
+    DD_CHECK(ws_bytes >= need, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
+    const CachedPass cp = {cache, (char*)codes, scales, map, pattern, max_new, max_kv, (char*)ws + fwd, need - fwd};
+    return run_forward(cfg, params, z_t, 1, map->T, alpha_t, logits, ld, (char*)ws, (hipStream_t)stream, nullptr,
+                       nullptr, nullptr, lora_gate, nullptr, 0, nullptr, 0, 0, nullptr, &cp);
 }
 
 dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V, void* out,

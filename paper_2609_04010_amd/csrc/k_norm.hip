@@ -57,8 +57,26 @@ DD_DEV void ln_row(const float (&x)[NPL], int lane, int d, const W* g, const W* 
     }
 }
 
+// Token and position of a row: position row % L, or row_pos[row] (below L) of a pass over a cached
+// context, where a negative position marks a row of padding: its token is not looked at.
+DD_DEV void embed_ids(const int32_t* z, const int32_t* row_pos, int64_t row, int L, int n_tok, int lane,
+                      int32_t* err, int& id, int& l) {
+    id = z[row];
+    l = row_pos ? row_pos[row] : (int)(row % L);
+    if (l < 0) id = l = 0;
+    if (l >= L) {
+        if (lane == 0 && err) atomicOr(err, DD_DEVERR_CACHE);
+        l = L - 1;
+    }
+    if (id < 0 || id >= n_tok) {
+        if (lane == 0 && err) atomicOr(err, DD_DEVERR_TOKEN);
+        id = id < 0 ? 0 : n_tok - 1;
+    }
+}
+
 template <typename W, int NPL, bool RMS>
-__global__ __launch_bounds__(256) void embed_ln_kernel(const int32_t* z, int64_t rows, int L,
+__global__ __launch_bounds__(256) void embed_ln_kernel(const int32_t* z, const int32_t* row_pos,
+                                                       int64_t rows, int L,
                                                        int n_tok, const W* tok, const W* pos,
                                                        const float* temb, const W* g, const W* b,
                                                        float eps, float* h, W* xln, int64_t ldo,
@@ -67,12 +85,8 @@ __global__ __launch_bounds__(256) void embed_ln_kernel(const int32_t* z, int64_t
     const int lane = threadIdx.x & 63;
     if (row >= rows) return;
     constexpr int d = NPL * 64;
-    int id = z[row];
-    if (id < 0 || id >= n_tok) {
-        if (lane == 0 && err) atomicOr(err, DD_DEVERR_TOKEN);
-        id = id < 0 ? 0 : n_tok - 1;
-    }
-    const int l = (int)(row % L);
+    int id, l;
+    embed_ids(z, row_pos, row, L, n_tok, lane, err, id, l);
     float x[NPL];
 #pragma unroll
     for (int k = 0; k < NPL; ++k) {
@@ -225,7 +239,8 @@ __global__ __launch_bounds__(256) void ln_bf16_v4_kernel(const float* h, int64_t
 // Embedding + first LayerNorm, bf16, d % 256 == 0: token and position rows read four features at a
 // time (8-byte loads), the residual row written with 16-byte stores.
 template <int NV, bool RMS>
-__global__ __launch_bounds__(256) void embed_ln_bf16_v4_kernel(const int32_t* z, int64_t rows, int L,
+__global__ __launch_bounds__(256) void embed_ln_bf16_v4_kernel(const int32_t* z, const int32_t* row_pos,
+                                                               int64_t rows, int L,
                                                                int n_tok, const bf16_t* tok,
                                                                const bf16_t* pos, const float* temb,
                                                                const bf16_t* g, const bf16_t* b, float eps,
@@ -235,12 +250,8 @@ __global__ __launch_bounds__(256) void embed_ln_bf16_v4_kernel(const int32_t* z,
     const int lane = threadIdx.x & 63;
     if (row >= rows) return;
     constexpr int d = NV * 256;
-    int id = z[row];
-    if (id < 0 || id >= n_tok) {
-        if (lane == 0 && err) atomicOr(err, DD_DEVERR_TOKEN);
-        id = id < 0 ? 0 : n_tok - 1;
-    }
-    const int l = (int)(row % L);
+    int id, l;
+    embed_ids(z, row_pos, row, L, n_tok, lane, err, id, l);
     const uint2* tv = (const uint2*)(tok + (int64_t)id * d);
     const uint2* pv = (const uint2*)(pos + (int64_t)l * d);
     float4* hr = (float4*)(h + row * d);
@@ -266,14 +277,14 @@ __global__ __launch_bounds__(256) void embed_ln_bf16_v4_kernel(const int32_t* z,
 #define DD_NPL_CASES(X) X(1) X(2) X(4) X(8) X(12) X(16) X(24) X(32)
 
 template <typename W, bool RMS>
-dd_status launch_embed_ln_t(const int32_t* z, int64_t rows, int L, int n_tok, int d, const void* tok,
+dd_status launch_embed_ln_t(const int32_t* z, const int32_t* row_pos, int64_t rows, int L, int n_tok, int d, const void* tok,
                             const void* pos, const float* temb, const void* g, const void* b,
                             float eps, float* h, void* xln, int64_t ldo, int32_t* err, hipStream_t s) {
     const dim3 grid((unsigned)ceil_div(rows, 4)), blk(256);
     switch (d / 64) {
 #define X(n)                                                                                     \
     case n:                                                                                      \
-        launch_k((embed_ln_kernel<W, n, RMS>), grid, blk, 0, s, z, rows, L, n_tok,     \
+        launch_k((embed_ln_kernel<W, n, RMS>), grid, blk, 0, s, z, row_pos, rows, L, n_tok,     \
                            (const W*)tok, (const W*)pos, temb, (const W*)g, (const W*)b, eps, h,  \
                            (W*)xln, ldo, err);                                                   \
         break;
@@ -300,7 +311,7 @@ static bool nv_supported(int d) {
 }
 
 template <bool RMS>
-void launch_embed_ln_v4(int d, dim3 grid, const int32_t* z, int64_t rows, int L, int n_tok,
+void launch_embed_ln_v4(int d, dim3 grid, const int32_t* z, const int32_t* row_pos, int64_t rows, int L, int n_tok,
                         const bf16_t* tk, const bf16_t* ps, const float* temb, const bf16_t* g,
                         const bf16_t* b, float eps, float* h, bf16_t* o, int64_t ldo, int32_t* err,
                         hipStream_t s) {
@@ -308,7 +319,7 @@ void launch_embed_ln_v4(int d, dim3 grid, const int32_t* z, int64_t rows, int L,
     switch (d / 256) {
 #define X(n)                                                                                              \
     case n:                                                                                               \
-        launch_k((embed_ln_bf16_v4_kernel<n, RMS>), grid, blk, 0, s, z, rows, L, n_tok, tk, ps, temb, g, \
+        launch_k((embed_ln_bf16_v4_kernel<n, RMS>), grid, blk, 0, s, z, row_pos, rows, L, n_tok, tk, ps, temb, g, \
                  b, eps, h, o, ldo, err);                                                                 \
         break;
         DD_NV_CASES(X)
@@ -319,22 +330,22 @@ void launch_embed_ln_v4(int d, dim3 grid, const int32_t* z, int64_t rows, int L,
 dd_status launch_embed_ln(int dtype, int norm, const int32_t* z, int64_t rows, int L, int n_tok, int d,
                           const void* tok, const void* pos, const float* temb, const void* g,
                           const void* b, float eps, float* h, void* xln, int64_t ldo, int32_t* err,
-                          hipStream_t s) {
+                          hipStream_t s, const int32_t* row_pos) {
     const bool rms = norm == DD_NORM_RMS;
     ProfScope ps(KC_EMBED_LN, s);
     if (dtype == DD_BF16 && nv_supported(d) && ldo % 4 == 0) {
         const dim3 grid((unsigned)ceil_div(rows, 4));
         const bf16_t *tk = (const bf16_t*)tok, *ps_ = (const bf16_t*)pos, *gg = (const bf16_t*)g, *bb = (const bf16_t*)b;
         bf16_t* o = (bf16_t*)xln;
-        if (rms) launch_embed_ln_v4<true>(d, grid, z, rows, L, n_tok, tk, ps_, temb, gg, bb, eps, h, o, ldo, err, s);
-        else launch_embed_ln_v4<false>(d, grid, z, rows, L, n_tok, tk, ps_, temb, gg, bb, eps, h, o, ldo, err, s);
+        if (rms) launch_embed_ln_v4<true>(d, grid, z, row_pos, rows, L, n_tok, tk, ps_, temb, gg, bb, eps, h, o, ldo, err, s);
+        else launch_embed_ln_v4<false>(d, grid, z, row_pos, rows, L, n_tok, tk, ps_, temb, gg, bb, eps, h, o, ldo, err, s);
         return launch_status("embed_ln");
     }
     if (dtype == DD_BF16)
-        return rms ? launch_embed_ln_t<bf16_t, true>(z, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s)
-                   : launch_embed_ln_t<bf16_t, false>(z, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s);
-    return rms ? launch_embed_ln_t<float, true>(z, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s)
-               : launch_embed_ln_t<float, false>(z, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s);
+        return rms ? launch_embed_ln_t<bf16_t, true>(z, row_pos, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s)
+                   : launch_embed_ln_t<bf16_t, false>(z, row_pos, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s);
+    return rms ? launch_embed_ln_t<float, true>(z, row_pos, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s)
+               : launch_embed_ln_t<float, false>(z, row_pos, rows, L, n_tok, d, tok, pos, temb, g, b, eps, h, xln, ldo, err, s);
 }
 
 template <typename W, bool RMS>

@@ -162,10 +162,11 @@ dd_status launch_init(void* dst, int64_t count, uint32_t id, double shift, int i
                       uint64_t seed, hipStream_t s);
 dd_status launch_temb(float* temb, int d, double tau, hipStream_t s);
 // norm: dd_norm (LayerNorm or RMSNorm; b is not read under RMSNorm)
+// row_pos (device, nullable): position of each row, -1 for padding, all below L (else row % L)
 dd_status launch_embed_ln(int dtype, int norm, const int32_t* z, int64_t rows, int L, int n_tok, int d,
                           const void* tok, const void* pos, const float* temb, const void* g,
                           const void* b, float eps, float* h, void* xln, int64_t ldo, int32_t* err,
-                          hipStream_t s);
+                          hipStream_t s, const int32_t* row_pos = nullptr);
 // Partials of a split residual projection: a row is h + slab[0] + .. + slab[n - 1] (each [rows][d]),
 // written back to h_out (nullable) and normalised.
 struct LnSlabs {

@@ -139,3 +139,34 @@ def test_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(ValueError):
         dd.logits_edit(torch.zeros(4, 64), "fp32", 64, 4, 32, torch.zeros(4, 64), history=torch.zeros(4, dtype=torch.int32))
     assert cc.n_blocks == 8
+
+
+def _cached(cfg=None, c=None, m=None, **kw):
+    import workloads
+    cfg = dd.make_config(dict(workloads.model_cfg(2), **(cfg or {})))
+    a = dict(params=FAKE, z=FAKE, alpha=1.0, codes=FAKE, scales=FAKE, pattern=1, max_new=4, max_kv=256, gate=None, logits=FAKE,
+             ld=50304, ws=FAKE, wsb=1 << 40)
+    a.update(kw)
+    return dd.lib().dd_denoise_forward_cached(
+        REF(cfg), a["params"], a["z"], a["alpha"], REF(c or _cache(n_kv_heads=12)), a["codes"], a["scales"], REF(m or _map()),
+        a["pattern"], a["max_new"], a["max_kv"], a["gate"], a["logits"], a["ld"], a["ws"], a["wsb"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(cfg=dict(d_model=770)), 1), (dict(cfg=dict(n_heads=24)), 6), (dict(c=_cache(n_kv_heads=6)), 2),
+    (dict(c=_cache(n_kv_heads=12, head_dim=32)), 2), (dict(c=_cache(n_kv_heads=12, block=40)), 6), (dict(m=_map(S=-1)), 1),
+    (dict(alpha=1.5), 1), (dict(pattern=0, codes=None), 1), (dict(pattern=3), 6), (dict(max_kv=257), 2), (dict(max_kv=1025), 2),
+    (dict(max_new=0), 1), (dict(gate=FAKE), 1), (dict(ld=50000), 2), (dict(ld=50257), 2), (dict(params=None), 1), (dict(z=None), 1),
+    (dict(scales=None), 1), (dict(logits=None), 1), (dict(ws=None), 1), (dict(ws=FAKE + 16), 1), (dict(logits=FAKE + 8), 1),
+    (dict(scales=FAKE + 4), 1), (dict(wsb=1000), 4)])
+def test_cached_forward_refusals(kw, status):
+    assert _cached(**kw) == status
+
+
+def test_cached_workspace():
+    import workloads
+    cfg, c = workloads.model_cfg(2), _cache(n_kv_heads=12, n_blocks=100)
+    n = dd.cached_workspace_bytes(cfg, c, 4, 64, 16, 1024)
+    assert n >= dd.workspace_bytes(cfg, 1, 64) + dd.cache_attention_workspace_bytes(c, 4, 64, 12, 16, 1024)
+    assert dd.cached_workspace_bytes(cfg, c, 4, 64, 16, 1025) == 0      # beyond max_len
+    assert _cached(m=_map(T=0, row_seq=None, row_pos=None, slots=None), logits=None, ws=None) == 0
