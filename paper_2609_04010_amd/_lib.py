@@ -464,21 +464,38 @@ def gaussian_latent_argmax(x, rows, V, alpha_tilde, sigma, seed, step, z_out, ro
 
 # ---------------------------------------------------------------- cached context
 
-def _here(device, name):
-    """The library runs on the current device: a tensor of another one is refused."""
-    if device.type != "cuda":
-        raise ValueError(f"{name} must be on the GPU, got {device}")
-    if device.index != _torch().cuda.current_device():
-        raise ValueError(f"{name} must be on the current GPU (cuda:{_torch().cuda.current_device()}), got {device}")
+# These calls are short on the GPU, so what a wrapper costs on the host is most of a small one: the current
+# device and its stream are looked up once per call, and each tensor in as few calls as the checks need.
+
+_here, _raw_stream = None, None
 
 
-def _dev(t, n, name, dtype):
-    """Device pointer of a contiguous tensor of at least n entries of `dtype` on the current GPU (0 for None)."""
+def _current():
+    """(index, stream) of the current GPU."""
+    global _here, _raw_stream
+    if _here is None:
+        torch = _torch()
+        torch.cuda.init()
+        _here = torch.cuda.current_device
+        # torch's own accessor without the Stream object around it, where this torch has it
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    dev = _here()
+    return dev, _raw_stream(dev)
+
+
+def _other_device(t, dev, name):
+    raise ValueError(f"{name} must be on the current GPU (cuda:{dev}), got {t.device}")
+
+
+def _dev(t, dev, n, name, dtype):
+    """Device pointer of a contiguous tensor of at least n entries of `dtype` on GPU `dev` (None for None)."""
     if t is None:
         return None
     if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    _here(t.device, name)
+    if t.get_device() != dev:
+        _other_device(t, dev, name)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if t.numel() < n:
@@ -486,19 +503,21 @@ def _dev(t, n, name, dtype):
     return t.data_ptr()
 
 
-def _rows(t, n, width, name, dtype=None):
+def _rows(t, dev, n, width, name, dtype):
     """(device pointer, row stride) of a tensor [n or more][width or more] with neighbouring columns: a view of
     columns of wider rows will do."""
-    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [{n}, {width}] with neighbouring columns, got {tuple(t.shape)} "
-                         f"with strides {t.stride()}")
-    if dtype is not None and t.dtype is not dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    _here(t.device, name)
-    if t.shape[0] > 1 and t.stride(0) < width:
-        raise ValueError(f"{name}: rows overlap (stride {t.stride(0)} for {width} columns)")
-    ld = t.stride(0)
-    if t.shape[0] <= 1:      # the stride of a single row says nothing
+    if t.get_device() != dev:
+        _other_device(t, dev, name)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if rows < n or cols < width or (unit != 1 and cols > 1) or (rows > 1 and ld < width):
+        raise ValueError(f"{name} must be [{n}, {width}] with neighbouring columns and rows that do not overlap, got "
+                         f"{(rows, cols)} with strides {(ld, unit)}")
+    if rows <= 1:      # the stride of a single row says nothing
         unit = 16 // t.element_size()
         ld = (width + unit - 1) // unit * unit
     return t.data_ptr(), ld
@@ -535,16 +554,25 @@ class CacheMap:
         i32 = _torch().int32
         if block_table.dim() != 2:
             raise ValueError("block_table must be [S, ld_table]")
+        if block_table.get_device() < 0:
+            raise ValueError(f"block_table must be on the GPU, got {block_table.device}")
         S, ld = block_table.shape
         T = row_seq.numel()
         self.block_table, self.held, self.kv_len, self.row_start = block_table, held, kv_len, row_start
         self.row_seq, self.row_pos, self.slots = row_seq, row_pos, slots
         self.S, self.T, self.ld_table = S, T, ld
-        self.device = block_table.device
-        self.struct = DDCacheMap(S, T, ld, _dev(block_table, S * ld, "block_table", i32), _dev(held, S, "held", i32),
-                                 _dev(kv_len, S, "kv_len", i32), _dev(row_start, S + 1, "row_start", i32),
-                                 _dev(row_seq, T, "row_seq", i32), _dev(row_pos, T, "row_pos", i32),
-                                 _dev(slots, T, "slots", i32))
+        self.device = dev = block_table.get_device()
+        self.struct = DDCacheMap(S, T, ld, _dev(block_table, dev, S * ld, "block_table", i32), _dev(held, dev, S, "held", i32),
+                                 _dev(kv_len, dev, S, "kv_len", i32), _dev(row_start, dev, S + 1, "row_start", i32),
+                                 _dev(row_seq, dev, T, "row_seq", i32), _dev(row_pos, dev, T, "row_pos", i32),
+                                 _dev(slots, dev, T, "slots", i32))
+        self.ref = ctypes.byref(self.struct)
+
+    def on(self, dev):
+        """The struct's reference, for calls on GPU `dev`."""
+        if self.device != dev:
+            raise ValueError(f"the map must be on the current GPU (cuda:{dev}), got cuda:{self.device}")
+        return self.ref
 
     @classmethod
     def empty(cls, S, T, ld_table, device="cuda"):
@@ -555,34 +583,33 @@ class CacheMap:
 
 
 def cache_plan(cc, m, seq_len, n_new, held, free_blocks, n_free, n_free_out, dev_err=None):
-    i32 = _torch().int32
-    _here(m.device, "map")
+    i32, S = _torch().int32, m.S
+    dev, stream = _current()
     _check(lib().dd_cache_plan(
-        ctypes.byref(cc), ctypes.byref(m.struct), _dev(seq_len, m.S, "seq_len", i32), _dev(n_new, m.S, "n_new", i32),
-        _dev(held, m.S, "held", i32), _dev(free_blocks, cc.n_blocks, "free_blocks", i32), _dev(n_free, 1, "n_free", i32),
-        _dev(n_free_out, 1, "n_free_out", i32), _dev(dev_err, 1, "dev_err", i32), _stream()))
+        ctypes.byref(cc), m.on(dev), _dev(seq_len, dev, S, "seq_len", i32), _dev(n_new, dev, S, "n_new", i32),
+        _dev(held, dev, S, "held", i32), _dev(free_blocks, dev, cc.n_blocks, "free_blocks", i32),
+        _dev(n_free, dev, 1, "n_free", i32), _dev(n_free_out, dev, 1, "n_free_out", i32),
+        _dev(dev_err, dev, 1, "dev_err", i32), stream))
 
 
-def _cache_ptrs(cc, codes, scales):
+def _cache_ptrs(cc, dev, codes, scales, layers=1):
     torch = _torch()
-    n = cc.n_blocks * cc.n_kv_heads * 2
-    if codes.dtype is torch.float8_e4m3fn:
-        codes = codes.view(torch.uint8)
-    return (_dev(codes, n * cc.block * cc.head_dim, "codes", torch.uint8), _dev(scales, n, "scales", torch.float32))
+    n = layers * cc.n_blocks * cc.n_kv_heads * 2
+    t = torch.uint8 if codes.dtype is not torch.float8_e4m3fn else torch.float8_e4m3fn
+    return (_dev(codes, dev, n * cc.block * cc.head_dim, "codes", t), _dev(scales, dev, n, "scales", torch.float32))
 
 
 def cache_append(cc, codes, scales, m, k, v, dev_err=None):
     """dd_cache_append; k and v are [T, n_kv_heads head_dim], of one type and row stride (views of packed rows)."""
-    _here(m.device, "map")
-    w = cc.n_kv_heads * cc.head_dim
-    code = _float_code(k, "k")
-    pk, ld = _rows(k, m.T, w, "k")
-    pv, ldv = _rows(v, m.T, w, "v", k.dtype)
+    dev, stream = _current()
+    T, w, t = m.T, cc.n_kv_heads * cc.head_dim, k.dtype
+    pk, ld = _rows(k, dev, T, w, "k", t)
+    pv, ldv = _rows(v, dev, T, w, "v", t)
     if ld != ldv:
         raise ValueError(f"k and v must have one row stride, got {ld} and {ldv}")
-    pc, ps = _cache_ptrs(cc, codes, scales)
-    _check(lib().dd_cache_append(ctypes.byref(cc), pc, ps, ctypes.byref(m.struct), pk, pv, code, ld,
-                                 _dev(dev_err, 1, "dev_err", _torch().int32), _stream()))
+    pc, ps = _cache_ptrs(cc, dev, codes, scales)
+    _check(lib().dd_cache_append(ctypes.byref(cc), pc, ps, m.on(dev), pk, pv, _float_code(k, "k"), ld,
+                                 _dev(dev_err, dev, 1, "dev_err", _torch().int32), stream))
 
 
 def cache_attention_workspace_bytes(cc, S, T, n_heads, max_new, max_kv):
@@ -593,19 +620,16 @@ def cache_attention_workspace_bytes(cc, S, T, n_heads, max_new, max_kv):
 def cache_attention(cc, codes, scales, m, q, out, n_heads, max_new, max_kv, ws=None, pattern="causal",
                     softmax_scale=None, dev_err=None):
     """dd_cache_attention; q and out are [T, n_heads head_dim]; softmax_scale defaults to head_dim ** -0.5."""
-    _here(m.device, "map")
-    w = n_heads * cc.head_dim
-    code = _float_code(q, "q")
-    pq, ldq = _rows(q, m.T, w, "q")
-    po, ldo = _rows(out, m.T, w, "out", q.dtype)
-    pc, ps = _cache_ptrs(cc, codes, scales)
-    if ws is not None:
-        _here(ws.device, "ws")
+    dev, stream = _current()
+    T, w, t = m.T, n_heads * cc.head_dim, q.dtype
+    pq, ldq = _rows(q, dev, T, w, "q", t)
+    po, ldo = _rows(out, dev, T, w, "out", t)
+    pc, ps = _cache_ptrs(cc, dev, codes, scales)
+    pw, wb = (None, 0) if ws is None else (_dev(ws, dev, 0, "ws", ws.dtype), ws.numel() * ws.element_size())
     _check(lib().dd_cache_attention(
-        ctypes.byref(cc), pc, ps, ctypes.byref(m.struct), pq, ldq, po, ldo, code, int(n_heads), ATTN_PATTERNS[pattern],
-        float(softmax_scale if softmax_scale is not None else cc.head_dim ** -0.5), int(max_new), int(max_kv),
-        _ptr(ws, 0, "ws"), ws.numel() * ws.element_size() if ws is not None else 0,
-        _dev(dev_err, 1, "dev_err", _torch().int32), _stream()))
+        ctypes.byref(cc), pc, ps, m.on(dev), pq, ldq, po, ldo, _float_code(q, "q"), n_heads, ATTN_PATTERNS[pattern],
+        softmax_scale if softmax_scale is not None else cc.head_dim ** -0.5, max_new, max_kv, pw, wb,
+        _dev(dev_err, dev, 1, "dev_err", _torch().int32), stream))
 
 
 def cached_workspace_bytes(cfg, cc, S, T, max_new, max_kv):
@@ -618,18 +642,16 @@ def denoise_forward_cached(cfg, params, z_t, alpha_t, cc, codes, scales, m, logi
     """dd_denoise_forward_cached; codes and scales hold the caches of the n_layers layers (cache_tensors with
     layers=n_layers)."""
     torch = _torch()
-    es = 2 if cfg["dtype"] == "bf16" else 4
     i32 = torch.int32
-    _here(m.device, "map")
-    n = cfg["n_layers"] * cc.n_blocks * cc.n_kv_heads * 2
-    if codes.dtype is torch.float8_e4m3fn:
-        codes = codes.view(torch.uint8)
+    dev, stream = _current()
+    pc, ps = _cache_ptrs(cc, dev, codes, scales, cfg["n_layers"])
+    pw = _dev(ws, dev, 0, "ws", ws.dtype)
     _check(lib().dd_denoise_forward_cached(
-        ctypes.byref(make_config(cfg)), _ptr(params, param_bytes(cfg), "params"), _dev(z_t, m.T, "z_t", i32), float(alpha_t),
-        ctypes.byref(cc), _dev(codes, n * cc.block * cc.head_dim, "codes", torch.uint8), _dev(scales, n, "scales", torch.float32),
-        ctypes.byref(m.struct), ATTN_PATTERNS[pattern], int(max_new), int(max_kv), _dev(lora_gate, m.T, "lora_gate", i32),
-        _ptr(logits, es * m.T * ld, "logits"), int(ld),
-        _ptr(ws, cached_workspace_bytes(cfg, cc, m.S, m.T, max_new, max_kv), "ws"), ws.numel() * ws.element_size(), _stream()))
+        ctypes.byref(make_config(cfg)), _ptr(params, param_bytes(cfg), "params"), _dev(z_t, dev, m.T, "z_t", i32),
+        float(alpha_t), ctypes.byref(cc), pc, ps, m.on(dev), ATTN_PATTERNS[pattern], max_new, max_kv,
+        _dev(lora_gate, dev, m.T, "lora_gate", i32),
+        _dev(logits, dev, m.T * ld, "logits", torch.bfloat16 if cfg["dtype"] == "bf16" else torch.float32), ld,
+        pw, ws.numel() * ws.element_size(), stream))
 
 
 def logits_edit(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, history=None, hist_len=None, repetition=None,
@@ -639,24 +661,34 @@ def logits_edit(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, history=
     torch = _torch()
     i32, f32 = torch.int32, torch.float32
     t = torch.bfloat16 if logits_dtype == "bf16" else f32
+    dev, stream = _current()
     n_seq = -(-rows // rows_per_seq) if rows_per_seq > 0 else 0
-    for name, x in (("history", history), ("bias_ids", bias_ids), ("bias_values", bias_values), ("allow", allow)):
-        if x is not None and x.dim() != 2:
-            raise ValueError(f"{name} must have two dimensions")
-    if bias_ids is not None and bias_values is not None and bias_ids.shape != bias_values.shape:
-        raise ValueError(f"bias_ids {tuple(bias_ids.shape)} and bias_values {tuple(bias_values.shape)} differ")
-    lh = history.shape[1] if history is not None else 0
-    nb = bias_ids.shape[1] if bias_ids is not None else 0
-    na, la = allow.shape if allow is not None else (0, 0)
+    lh = nb = na = la = 0
+    if history is not None:
+        _two_dims(history, "history")
+        lh = history.shape[1]
+    if bias_ids is not None:
+        _two_dims(bias_ids, "bias_ids")
+        nb = bias_ids.shape[1]
+        if bias_values is None or bias_values.shape != bias_ids.shape:
+            raise ValueError("bias_values must have the shape of bias_ids")
+    if allow is not None:
+        _two_dims(allow, "allow")
+        na, la = allow.shape
     e = DDLogitsEdits(
-        _dev(history, n_seq * lh, "history", i32), lh, _dev(hist_len, rows, "hist_len", i32),
-        _dev(repetition, n_seq, "repetition", f32), _dev(presence, n_seq, "presence", f32),
-        _dev(frequency, n_seq, "frequency", f32), _dev(bias_ids, n_seq * nb, "bias_ids", i32),
-        _dev(bias_values, n_seq * nb, "bias_values", f32), nb, _dev(allow, na * la, "allow", i32), la, na,
-        _dev(allow_id, rows, "allow_id", i32))
+        _dev(history, dev, n_seq * lh, "history", i32), lh, _dev(hist_len, dev, rows, "hist_len", i32),
+        _dev(repetition, dev, n_seq, "repetition", f32), _dev(presence, dev, n_seq, "presence", f32),
+        _dev(frequency, dev, n_seq, "frequency", f32), _dev(bias_ids, dev, n_seq * nb, "bias_ids", i32),
+        _dev(bias_values, dev, n_seq * nb, "bias_values", f32), nb, _dev(allow, dev, na * la, "allow", i32), la, na,
+        _dev(allow_id, dev, rows, "allow_id", i32))
     _check(lib().dd_logits_edit(
-        _dev(logits, rows * ld, "logits", t), dtype_code(logits_dtype), int(ld), int(rows), int(V),
-        _dev(out, rows * ld, "out", t), int(rows_per_seq), ctypes.byref(e), _dev(dev_err, 1, "dev_err", i32), _stream()))
+        _dev(logits, dev, rows * ld, "logits", t), dtype_code(logits_dtype), ld, rows, V, _dev(out, dev, rows * ld, "out", t),
+        rows_per_seq, ctypes.byref(e), _dev(dev_err, dev, 1, "dev_err", i32), stream))
+
+
+def _two_dims(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
 
 
 def workspace_reset(ws):

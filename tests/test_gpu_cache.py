@@ -452,3 +452,35 @@ def test_attention_is_the_same_from_call_to_call_and_in_a_graph():
         step(x, a, ws[0])
         torch.cuda.synchronize()
         assert torch.equal(a, os_), i
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    torch = torch_or_skip()
+    cc, m = dd.cache_config(4, 32, 2, 64), dd.CacheMap.empty(2, 8, 2)
+    codes, scales = dd.cache_tensors(cc)
+    x = torch.zeros((8, 128), device="cuda")
+    z = dev_i32(torch, [0, 0])
+    bad = [(TypeError, lambda: dd.cache_append(cc, codes, scales, m, x, x.bfloat16())),
+           (TypeError, lambda: dd.cache_append(cc, codes, scales, m, x.half(), x.half())),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x[:7], x)),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x[:, :120], x[:, :120])),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x, torch.zeros((8, 256), device="cuda"))),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x[:1].expand(8, 128), x[:1].expand(8, 128))),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x.t(), x.t())),
+           (ValueError, lambda: dd.cache_append(cc, codes, scales, m, x.cpu(), x.cpu())),
+           (ValueError, lambda: dd.cache_append(cc, codes[:3], scales, m, x, x)),
+           (TypeError, lambda: dd.cache_append(cc, codes, scales.double(), m, x, x)),
+           (ValueError, lambda: dd.cache_attention(cc, codes, scales, m, x, x[:, :64].contiguous(), 2, 4, 64)),
+           (dd.DDError, lambda: dd.cache_attention(cc, codes, scales, m, x, x.clone(), 2, 4, 65)),
+           (KeyError, lambda: dd.cache_attention(cc, codes, scales, m, x, x.clone(), 2, 4, 64, pattern="none")),
+           (ValueError, lambda: dd.cache_plan(cc, m, z[:1], z, z, dev_i32(torch, [0] * 4), z, z)),
+           (TypeError, lambda: dd.cache_plan(cc, m, z.long(), z, z, dev_i32(torch, [0] * 4), z, z)),
+           (ValueError, lambda: dd.logits_edit(x, "fp32", 128, 8, 100, x, history=z)),
+           (ValueError, lambda: dd.logits_edit(x, "fp32", 128, 8, 100, x, bias_ids=z[None])),
+           (ValueError, lambda: dd.logits_edit(x, "fp32", 128, 9, 100, x)),
+           (ValueError, lambda: dd.logits_edit(x, "fp32", 128, 8, 100, x, hist_len=z)),
+           (TypeError, lambda: dd.logits_edit(x, "bf16", 128, 8, 100, x))]
+    for i, (what, call) in enumerate(bad):
+        with pytest.raises(what):
+            call()
+            pytest.fail(f"call {i} was not refused")
