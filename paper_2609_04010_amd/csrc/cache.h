@@ -75,13 +75,15 @@ struct CacheAttnArgs {
     float* part;          // nsplit > 1: [T][Hq][nsplit][dh] sums, then [T][Hq][nsplit][2] (maximum, sum)
     int32_t* err;
 };
-// How a call's keys are cut: wavefronts of a workgroup per query tile and tokens per workgroup.
+// How a call is cut: shape of a workgroup (an index into the launcher's table), column tiles of a key head,
+// tokens per workgroup and how many such pieces max_kv has, bytes of partial results.
 struct CacheAttnPlan {
-    int kw, chunk, nsplit;
+    int shape, chunk, nsplit;
+    int64_t tiles;
     size_t ws;
 };
 CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int dh, int32_t max_new, int32_t max_kv);
-dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, int kw, hipStream_t s);
+dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
 struct EditArgs {
     const void* logits;

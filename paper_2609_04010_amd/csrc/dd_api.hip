@@ -956,12 +956,11 @@ static dd_status cache_attn_check(const dd_cache* cache, int32_t S, int32_t T, i
     DD_CHECK(S >= 0 && T >= 0 && n_heads > 0 && max_new > 0 && max_kv > 0, DD_E_ARG,
              "n_heads, max_new and max_kv must be positive");
     DD_CHECK(n_heads % cache->n_kv_heads == 0, DD_E_SHAPE, "n_heads must be a multiple of n_kv_heads");
-    DD_CHECK((int64_t)max_kv <= INT32_MAX - 256 && (int64_t)max_new * n_heads <= INT32_MAX - 256, DD_E_UNSUPPORTED,
+    DD_CHECK(max_kv <= (1 << 30) && (int64_t)max_new * n_heads <= (1 << 30), DD_E_UNSUPPORTED,
              "max_kv or max_new * n_heads too large");
     if (S == 0 || T == 0) return DD_OK;
     const CacheAttnPlan p = cache_attn_plan(S, T, cache->n_kv_heads, n_heads, cache->head_dim, max_new, max_kv);
-    const int64_t tiles = ceil_div((int64_t)max_new * (n_heads / cache->n_kv_heads), 32 * (4 / p.kw));
-    const double wgs = ((double)S * cache->n_kv_heads * p.nsplit + 8) * (double)tiles;
+    const double wgs = ((double)S * cache->n_kv_heads * p.nsplit + 8) * (double)p.tiles;
     DD_CHECK(wgs < 2147483647.0 && (double)S * max_new * n_heads < 2147483647.0, DD_E_UNSUPPORTED,
              "too many workgroups: S * max_new * n_heads is too large");
     return DD_OK;
@@ -1000,7 +999,7 @@ dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const flo
                        n_heads / cache->n_kv_heads, pattern == DD_ATTN_CAUSAL,
                        (float)(softmax_scale * 1.4426950408889634), max_new, max_kv, p.chunk, p.nsplit, (float*)ws,
                        dev_err};
-    return launch_cache_attn(dtype, a, p.kw, (hipStream_t)stream);
+    return launch_cache_attn(dtype, a, p, (hipStream_t)stream);
 }
 
 // Checks of a pass over a cached context that need no buffers.

@@ -19,9 +19,14 @@
 // fp32 rows: q (and the probabilities) are taken as the sum of three bf16 numbers of 8 bits each, which is
 // exact, one product each.
 //
-// A workgroup is four wavefronts: KW of them share a column tile and take every KW-th tile of tokens, their
-// results meet in LDS; 4 / KW column tiles side by side.  Long caches are cut into pieces of `chunk` tokens
-// over workgroups whose partial results cache_attn_join_kernel adds.
+// KW wavefronts of a workgroup share a column tile and take every KW-th tile of tokens; their results meet in
+// LDS.  Where that leaves CUs idle, long caches are cut into pieces of `chunk` tokens over workgroups whose
+// partial results cache_attn_join_kernel adds.
+//
+// Bound: few columns per key head, by the bytes of the cache (32 rows, 8 heads of 128, 16384 to 32768 tokens:
+// 1.61 GB in 302 us, 5.3 TB/s, where reading such blocks and nothing else reaches 6.0; 64 x 16 rows, 12 heads of 64,
+// 2048 to 4112 tokens: 303 MB in 56 us, 5.4 TB/s); many columns, by the vector instructions between the products
+// (about 590 cycles per 32 x 32 tile, 256 of matrix instructions: prompts of 4 x 2048 rows, 64 GFLOP in 102 us).
 #include <math.h>
 
 #include <algorithm>
@@ -86,20 +91,38 @@ template <> DD_DEV void store4<float>(float* p, float4 v) { *(float4*)p = v; }
 
 DD_DEV float4 scaled(float4 v, float f) { return make_float4(v.x * f, v.y * f, v.z * f, v.w * f); }
 
-template <typename T, int DH, int KW>
-__global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
-    constexpr int CW = 4 / KW, NS = sizeof(T) == 4 ? 3 : 1, KS = DH / 16, MT = DH / 32;
+// maximum of a lane and the one 32 from it, in both
+DD_DEV float max_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// KW wavefronts share a column tile, CW column tiles side by side, NB tiles of tokens in a wavefront's registers
+// (NB - 1 ahead of the one in work).
+template <typename T, int DH, int KW, int CW, int NB>
+__global__ __launch_bounds__(64 * KW * CW) void cache_attn_kernel(CacheAttnArgs a) {
+    constexpr int NS = sizeof(T) == 4 ? 3 : 1, KS = DH / 16, MT = DH / 32;
+    constexpr int WC = 32 * CW;   // columns of a workgroup
     const int lane = threadIdx.x & 63, g = lane >> 5, ln = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kw = wave % KW, cw = wave / KW;
 
-    // workgroup -> (sequence, key head, piece, column tiles): the column tiles of a piece, which read the
-    // same tokens, are 8 apart in launch order, so that one XCD's L2 serves them
-    const int ntile = (int)((a.max_new * (int64_t)a.G + 32 * CW - 1) / (32 * CW));
+    // workgroup -> (sequence, key head, piece, column tiles): an XCD (every eighth workgroup) has all column
+    // tiles of a piece, which read the same tokens; the last tiles, which see most, start first
+    const int ntile = (int)((a.max_new * (int64_t)a.G + WC - 1) / WC);
+    const int groups = a.S * a.c.H * a.nsplit, gx = (groups + 7) >> 3;
     const int slot = blockIdx.x >> 3;
-    const int group = slot / ntile * 8 + (blockIdx.x & 7), ct = ntile - 1 - slot % ntile;   // the longest first
-    if (group >= a.S * a.c.H * a.nsplit) return;
-    const int piece = group % a.nsplit, sh = group / a.nsplit, h = sh % a.c.H, s = sh / a.c.H;
+    const int group = slot % gx * 8 + (blockIdx.x & 7), ct = ntile - 1 - slot / gx;
+    if (group >= groups) return;
+    // (pieces outermost: the XCDs share every piece's workgroups, of which the last ones may have nothing to do)
+    const int nsh = a.S * a.c.H, piece = group / nsh, sh = group - piece * nsh, s = sh / a.c.H, h = sh - s * a.c.H;
+
+    // block numbers and scales of 64 blocks from block bw on, one per lane (-1: not to be read); the table may be
+    // read before the length is known
+    const int k0 = piece * a.chunk;
+    int bw = k0 >> a.c.log2p, id = -1;
+    float2 sc = make_float2(0.f, 0.f);
+    if (bw + lane < a.ld_table) id = a.table[(int64_t)s * a.ld_table + bw + lane];
 
     const int kv = a.kv_len[s], most = (int)min((int64_t)a.max_kv, (int64_t)a.ld_table * a.c.P);
     const int L = min(max(kv, 0), most);
@@ -109,27 +132,31 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
         (kv < 0 || kv > most || r1 - r0 > a.max_new))
         atomicOr(a.err, DD_DEVERR_CACHE);
     const int cols = n * a.G;
-    const int k0 = piece * a.chunk;
-    if (ct * CW * 32 >= cols || (piece > 0 && k0 >= L)) return;
+    if (ct * WC >= cols || (piece > 0 && k0 >= L)) return;
     const bool whole = L <= a.chunk;   // the sequence has this piece alone
+
+    auto scales = [&]() {
+        const bool in = (int64_t)(bw + lane) << a.c.log2p < L;
+        if (in && (id < 0 || id >= a.c.n_blocks) && a.err) atomicOr(a.err, DD_DEVERR_CACHE);
+        if (!in || id < 0 || id >= a.c.n_blocks) id = -1;
+        if (id >= 0) sc = *(const float2*)(a.scales + ((int64_t)id * a.c.H + h) * 2);
+    };
+    scales();
 
     // this lane's column: row of the sequence and query head, and how many tokens it sees
     const int col = (ct * CW + cw) * 32 + ln;
     const bool real = col < cols;
-    const int i = real ? col / a.G : 0, head = h * a.G + (real ? col % a.G : 0);
+    const int i = real ? col / a.G : 0, row = r0 + i, head = h * a.G + (real ? col - i * a.G : 0);
     int lim = L;
     if (real && a.causal) lim = min(max(kv - (r1 - r0) + i + 1, 0), L);
-    const int lo = wave_min_int(lim), hi = wave_max_int(real ? lim : 0);
-
     bf16x8 q[KS][NS];
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
         float x[8] = {};
         if (real) {
-            const T* p = (const T*)a.q + (int64_t)(r0 + i) * a.ldq + (int64_t)head * DH + (st >> 1) * 32 + g * 16 + (st & 1) * 8;
+            const T* p = (const T*)a.q + (int64_t)row * a.ldq + (int64_t)head * DH + (st >> 1) * 32 + g * 16 + (st & 1) * 8;
             if constexpr (NS == 1) {
-                const uint4 u = *(const uint4*)p;
-                q[st][0] = __builtin_bit_cast(bf16x8, u);
+                q[st][0] = __builtin_bit_cast(bf16x8, *(const uint4*)p);
                 continue;
             } else {
                 const float4 y = ((const float4*)p)[0], z = ((const float4*)p)[1];
@@ -139,157 +166,156 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
         }
         split8<NS>(x, q[st]);
     }
+    const int lo = wave_min_int(lim), hi = wave_max_int(real ? lim : 0);
 
     f32x16 o[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) o[mt] = f32x16{};
     float m = -INFINITY, l = 0.f;
 
-    const int k1 = min(k0 + a.chunk, hi), nt = k1 > k0 ? (k1 - k0 + 31) >> 5 : 0;
-    // block numbers and scales of 64 blocks from block bw on, one per lane (-1: not to be read)
-    int bw = 0, id = -1;
-    float2 sc = make_float2(0.f, 0.f);
-    auto window = [&](int first) {
-        bw = first;
-        id = -1;
-        const int b = first + lane;
-        if ((int64_t)b << a.c.log2p < L) {
-            id = a.table[(int64_t)s * a.ld_table + b];
-            if (id < 0 || id >= a.c.n_blocks) {
-                if (a.err) atomicOr(a.err, DD_DEVERR_CACHE);
-                id = -1;
-            }
-        }
-        if (id >= 0) sc = *(const float2*)(a.scales + ((int64_t)id * a.c.H + h) * 2);
-    };
     struct Tile {
-        uint4 k[DH / 32], v[MT];
-        float ks, vs;
-        bool ok;
+        uint4 k[MT], v[MT];
     };
     const int krow = 16 * (ln >> 2 & 1) + 4 * (ln >> 3) + (ln & 3);   // the token whose key this lane loads
-    auto fetch = [&](int t, Tile& x) {
-        const int key0 = k0 + 32 * t, b = key0 >> a.c.log2p;
-        if (b - bw >= 64) window(b);
-        const int blk = __builtin_amdgcn_readlane(id, b - bw);
-        x.ok = blk >= 0;
-        if (!x.ok) return;
-        x.ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), b - bw));
-        x.vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), b - bw));
+    const int koff = krow * DH + g * 16, voff = ln * 32 + g * 16;
+    // loads the tile of 32 tokens from key0 on (block 0's places where its block is not to be read)
+    auto fetch = [&](int key0, Tile& x) {
+        const int blk = max(__builtin_amdgcn_readlane(id, (key0 >> a.c.log2p) - bw), 0);
         const uint8_t* p = a.codes + cache_slab(a.c, DH, blk, h) + (int64_t)(key0 & (a.c.P - 1)) * DH;
         const uint8_t* pv = p + (int64_t)a.c.P * DH;
 #pragma unroll
-        for (int e = 0; e < DH / 32; ++e) x.k[e] = *(const uint4*)(p + krow * DH + e * 32 + g * 16);
+        for (int e = 0; e < MT; ++e) x.k[e] = *(const uint4*)(p + koff + e * 32);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x.v[mt] = *(const uint4*)(pv + (mt * 32 + ln) * 32 + g * 16);
+        for (int mt = 0; mt < MT; ++mt) x.v[mt] = *(const uint4*)(pv + voff + mt * 1024);
     };
 
-    window(k0 >> a.c.log2p);
-    Tile cur, nxt;
-    if (kw < nt) fetch(kw, cur);
-    for (int t = kw; t < nt; t += KW) {
-        nxt.ok = false;
-        if (t + KW < nt) fetch(t + KW, nxt);
-        if (cur.ok) {
-            f32x16 sT = {};
+    auto work = [&](int tile0, Tile& x) {
+        const int b = (tile0 >> a.c.log2p) - bw;
+        if (__builtin_amdgcn_readlane(id, b) < 0) return;
+        const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), b));
+        const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), b));
+        f32x16 sT = {};
 #pragma unroll
-            for (int st = 0; st < KS; ++st) {
-                const bf16x8 kf = half8(cur.k[st >> 1], st & 1, cur.ks);
+        for (int st = 0; st < KS; ++st) {
+            const bf16x8 kf = half8(x.k[st >> 1], st & 1, ks);
 #pragma unroll
-                for (int p = NS - 1; p >= 0; --p) sT = mfma32(kf, q[st][p], sT);
+            for (int p = NS - 1; p >= 0; --p) sT = mfma32(kf, q[st][p], sT);
+        }
+        const int key0 = tile0 + 16 * g;
+        if (tile0 + 32 > lo) {   // some column does not see the whole tile
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sT[r] = key0 + r < lim ? sT[r] : -INFINITY;
+            // NaN codes in places that not every column sees (or nobody: beyond the sequence's end)
+            // would reach every column as 0 * NaN: they leave V, and the columns that see one get it back
+            uint32_t any = 0;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint4& u = x.v[mt];
+                any |= ((u.x & 0x7F7F7F7Fu) + 0x01010101u) | ((u.y & 0x7F7F7F7Fu) + 0x01010101u) |
+                       ((u.z & 0x7F7F7F7Fu) + 0x01010101u) | ((u.w & 0x7F7F7F7Fu) + 0x01010101u);
             }
-            const int key0 = k0 + 32 * t + 16 * g;
-            const bool edge = k0 + 32 * t + 32 > lo;   // some column does not see the whole tile
-            if (edge) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sT[r] = key0 + r < lim ? sT[r] : -INFINITY;
-            }
-            float tm = sT[0];
-#pragma unroll
-            for (int r = 1; r < 16; ++r) tm = fmaxf(tm, sT[r]);
-            tm = fmaxf(tm, __shfl_xor(tm, 32, 64)) * a.scale_log2;
-            // the reference moves only where a score passes it by 2^8: sums stay far inside fp32
-            if (__any(tm > m + 8.f)) {
-                const float mn = fmaxf(m, tm), f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                m = mn;
-                l *= f;
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[mt][r] *= f;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-            float p[16];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                p[r] = __builtin_amdgcn_exp2f(fmaf(sT[r], a.scale_log2, -ref));
-                l += p[r];
-            }
-            if (edge) {
-                // NaN codes in places that not every column sees (or nobody: beyond the sequence's end)
-                // would reach every column as 0 * NaN: they leave V, and the columns that see one get it back
-                uint32_t any = 0;
+            if (__any((any & 0x80808080u) != 0)) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    const uint4& u = cur.v[mt];
-                    any |= ((u.x & 0x7F7F7F7Fu) + 0x01010101u) | ((u.y & 0x7F7F7F7Fu) + 0x01010101u) |
-                           ((u.z & 0x7F7F7F7Fu) + 0x01010101u) | ((u.w & 0x7F7F7F7Fu) + 0x01010101u);
-                }
-                if (__any((any & 0x80808080u) != 0)) {
-                    float see[16];
+                    uint32_t u[4] = {x.v[mt].x, x.v[mt].y, x.v[mt].z, x.v[mt].w}, w[4];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) see[r] = key0 + r < lim ? 1.f : 0.f;
-                    bf16x8 sb[2][1];
-                    split8<1>(*(const float(*)[8])see, sb[0]);
-                    split8<1>(*(const float(*)[8])(see + 8), sb[1]);
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        uint32_t u[4] = {cur.v[mt].x, cur.v[mt].y, cur.v[mt].z, cur.v[mt].w}, w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t b = (((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
-                            u[e] &= ~(b * 0xFFu);
-                            w[e] = b * 0x38u;   // 1.0
-                        }
-                        cur.v[mt] = make_uint4(u[0], u[1], u[2], u[3]);
-                        f32x16 cnt = {};
-                        cnt = mfma32(cvt8(w[0], w[1], 1.f), sb[0][0], cnt);
-                        cnt = mfma32(cvt8(w[2], w[3], 1.f), sb[1][0], cnt);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[mt][r] += cnt[r] > 0.f ? NAN : 0.f;
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t nan = (((u[e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+                        u[e] &= ~(nan * 0xFFu);
+                        w[e] = nan * 0x38u;   // 1.0
                     }
-                }
-            }
+                    x.v[mt] = make_uint4(u[0], u[1], u[2], u[3]);
+                    f32x16 cnt = {};
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                float x[8];
+                    for (int st = 0; st < 2; ++st) {
+                        float see[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = p[8 * st + e];
-                bf16x8 pf[NS];
-                split8<NS>(x, pf);
+                        for (int e = 0; e < 8; ++e) see[e] = key0 + 8 * st + e < lim ? 1.f : 0.f;
+                        bf16x8 sb[1];
+                        split8<1>(see, sb);
+                        cnt = mfma32(cvt8(w[2 * st], w[2 * st + 1], 1.f), sb[0], cnt);
+                    }
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const bf16x8 vf = half8(cur.v[mt], st, cur.vs);
-#pragma unroll
-                    for (int e = NS - 1; e >= 0; --e) o[mt] = mfma32(vf, pf[e], o[mt]);
+                    for (int r = 0; r < 16; ++r) o[mt][r] += cnt[r] > 0.f ? NAN : 0.f;
                 }
             }
         }
-        cur = nxt;
+        float tm = sT[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) tm = fmaxf(tm, sT[r]);
+        tm = max_halves(tm) * a.scale_log2;
+        // the reference moves only where a score passes it by 2^8: sums stay far inside fp32
+        if (__any(tm > m + 8.f)) {
+            const float mn = fmaxf(m, tm), f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[mt][r] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf(sT[8 * st + e], a.scale_log2, -ref));
+                l += p[e];
+            }
+            bf16x8 pf[NS];
+            split8<NS>(p, pf);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const bf16x8 vf = half8(x.v[mt], st, vs);
+#pragma unroll
+                for (int e = NS - 1; e >= 0; --e) o[mt] = mfma32(vf, pf[e], o[mt]);
+            }
+        }
+    };
+
+    // Tiles of a window of 64 blocks: this wavefront takes every KW-th.  Loads run NB - 1 tiles ahead and are
+    // issued on every path (past the window's end its last tile again), so that the wait for a tile's
+    // registers counts the younger loads and does not drain them.
+    const int k1 = min(k0 + a.chunk, hi);
+    for (int w0 = k0; w0 < k1;) {
+        const int w1 = (int)min((int64_t)k1, (int64_t)(bw + 64) << a.c.log2p);
+        const int last = w0 + ((w1 - w0 - 1) & ~31);
+        const int t0 = w0 + 32 * kw;
+        if (t0 <= last) {
+            Tile tile[NB];
+#pragma unroll
+            for (int b = 0; b < NB - 1; ++b) fetch(min(t0 + 32 * KW * b, last), tile[b]);
+            for (int t = t0; t <= last; t += 32 * KW * NB) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const int tb = t + 32 * KW * b;
+                    fetch(min(tb + 32 * KW * (NB - 1), last), tile[(b + NB - 1) % NB]);
+                    if (tb <= last) work(tb, tile[b]);
+                }
+            }
+        }
+        w0 = w1;
+        if (w0 < k1) {
+            bw = w0 >> a.c.log2p;
+            id = -1;
+            if (bw + lane < a.ld_table) id = a.table[(int64_t)s * a.ld_table + bw + lane];
+            scales();
+        }
     }
     l += __shfl_xor(l, 32, 64);
 
     // four consecutive features of a column, normalised into out or, of a cut sequence, as they are
-    auto put = [&](int row, int hd, int d, float4 v, float sum) {
+    auto put = [&](int rw, int hd, int d, float4 v, float sum) {
         if (whole) {
-            store4<T>((T*)a.out + (int64_t)row * a.ldo + (int64_t)hd * DH + d, scaled(v, sum == 0.f ? 0.f : 1.f / sum));
+            store4<T>((T*)a.out + (int64_t)rw * a.ldo + (int64_t)hd * DH + d, scaled(v, sum == 0.f ? 0.f : 1.f / sum));
         } else {
-            *(float4*)(a.part + (((int64_t)row * a.Hq + hd) * a.nsplit + piece) * DH + d) = v;
+            *(float4*)(a.part + (((int64_t)rw * a.Hq + hd) * a.nsplit + piece) * DH + d) = v;
         }
     };
-    auto put_ml = [&](int row, int hd, float mx, float sum) {
+    auto put_ml = [&](int rw, int hd, float mx, float sum) {
         float* ml = a.part + (int64_t)a.T * a.Hq * a.nsplit * DH;
-        *(float2*)(ml + (((int64_t)row * a.Hq + hd) * a.nsplit + piece) * 2) = make_float2(mx, sum);
+        *(float2*)(ml + (((int64_t)rw * a.Hq + hd) * a.nsplit + piece) * 2) = make_float2(mx, sum);
     };
     if constexpr (KW == 1) {
         if (!real) return;
@@ -297,55 +323,72 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(CacheAttnArgs a) {
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                put(r0 + i, head, mt * 32 + 2 * r + 4 * g, make_float4(o[mt][r], o[mt][r + 1], o[mt][r + 2], o[mt][r + 3]), l);
-        if (!whole && g == 0) put_ml(r0 + i, head, m, l);
+                put(row, head, mt * 32 + 2 * r + 4 * g, make_float4(o[mt][r], o[mt][r + 1], o[mt][r + 2], o[mt][r + 3]), l);
+        if (!whole && g == 0) put_ml(row, head, m, l);
     } else {
-        // the KW results of a column tile meet in LDS, 32 features at a time
-        constexpr int LDC = 36;   // floats per column: 16-byte rows whose starts fall on different banks
-        __shared__ float so[4][32][LDC];
-        __shared__ float sml[4][32][2];
+        // The KW results of a column tile meet in LDS: all features at once where the columns are few, else 32
+        // at a time.
+        constexpr int NT = 64 * KW * CW, LDC = 36, LDA = DH + 4;   // floats per column, 16-byte rows on different banks
+        constexpr int FEW = CW == 1 ? 32 * LDC / LDA : 0;
+        __shared__ __attribute__((aligned(16))) float so[KW * CW][32 * LDC];
+        __shared__ float sml[KW * CW][32][2];
         if (g == 0) {
             sml[wave][ln][0] = m;
             sml[wave][ln][1] = l;
+        }
+        auto join = [&](int c, int cl, int ld, int dl, int d) {   // column cl of tile c, four features from d on
+            const int cc = (ct * CW + c) * 32 + cl;
+            if (cc >= cols) return;
+            float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) mx = fmaxf(mx, sml[c * KW + k][cl][0]);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const float mk = sml[c * KW + k][cl][0], f = mk == mx ? 1.f : __builtin_amdgcn_exp2f(mk - mx);
+                const float4 y = *(const float4*)&so[c * KW + k][cl * ld + dl];
+                sum += sml[c * KW + k][cl][1] * f;
+                v.x += y.x * f; v.y += y.y * f; v.z += y.z * f; v.w += y.w * f;
+            }
+            const int j = cc / a.G, rw = r0 + j, hd = h * a.G + cc - j * a.G;
+            put(rw, hd, d, v, sum);
+            if (!whole && d == 0) put_ml(rw, hd, mx, sum);
+        };
+        const int here = min(cols - ct * WC, WC);
+        if (here <= FEW) {
+            if (real) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *(float4*)&so[wave][ln * LDA + mt * 32 + 2 * r + 4 * g] =
+                            make_float4(o[mt][r], o[mt][r + 1], o[mt][r + 2], o[mt][r + 3]);
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < here * (DH / 4); e += NT) join(0, e / (DH / 4), LDA, e % (DH / 4) * 4, e % (DH / 4) * 4);
+            return;
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt) __syncthreads();
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                *(float4*)&so[wave][ln][2 * r + 4 * g] = make_float4(o[mt][r], o[mt][r + 1], o[mt][r + 2], o[mt][r + 3]);
+                *(float4*)&so[wave][ln * LDC + 2 * r + 4 * g] = make_float4(o[mt][r], o[mt][r + 1], o[mt][r + 2], o[mt][r + 3]);
             __syncthreads();
-#pragma unroll
-            for (int c = 0; c < CW; ++c) {
-                const int cl = threadIdx.x >> 3, d = (threadIdx.x & 7) * 4, cc = (ct * CW + c) * 32 + cl;
-                if (cc >= cols) continue;
-                float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int k = 0; k < KW; ++k) mx = fmaxf(mx, sml[c * KW + k][cl][0]);
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int k = 0; k < KW; ++k) {
-                    const float mk = sml[c * KW + k][cl][0], f = mk == mx ? 1.f : __builtin_amdgcn_exp2f(mk - mx);
-                    const float4 y = *(const float4*)&so[c * KW + k][cl][d];
-                    sum += sml[c * KW + k][cl][1] * f;
-                    v.x += y.x * f; v.y += y.y * f; v.z += y.z * f; v.w += y.w * f;
-                }
-                const int row = r0 + cc / a.G, hd = h * a.G + cc % a.G;
-                put(row, hd, mt * 32 + d, v, sum);
-                if (!whole && mt == 0 && d == 0) put_ml(row, hd, mx, sum);
-            }
+            for (int e = threadIdx.x; e < 256 * CW; e += NT) join(e >> 8, e >> 3 & 31, LDC, (e & 7) * 4, mt * 32 + (e & 7) * 4);
         }
     }
 }
 
-// Adds the pieces of cut sequences: one wavefront per (row of a sequence, query head); lanes first hold one
-// piece's maximum and sum each (at most 64), then DH / 64 features.
+// Adds the pieces of cut sequences: one wavefront per (row of a sequence, query head).  Each lane holds one
+// piece's maximum and sum (at most 64 pieces); DH / 4 lanes then hold four features each of one piece, 256 / DH
+// pieces side by side.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnArgs a) {
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     const int64_t per = (int64_t)a.max_new * a.Hq;
-    const int s = (int)(item / per), i = (int)(item % per / a.Hq), head = (int)(item % a.Hq);
+    const int s = (int)(item / per), rem = (int)(item - s * per), i = rem / a.Hq, head = rem - i * a.Hq;
     if (s >= a.S) return;
     const int most = (int)min((int64_t)a.max_kv, (int64_t)a.ld_table * a.c.P);
     const int L = min(max(a.kv_len[s], 0), most), np = (L + a.chunk - 1) / a.chunk;
@@ -354,51 +397,83 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnArgs a) {
     const int64_t at = ((int64_t)(r0 + i) * a.Hq + head) * a.nsplit;
     const float* part = a.part + at * DH;
     const float2* ml = (const float2*)(a.part + (int64_t)a.T * a.Hq * a.nsplit * DH) + at;
+    constexpr int FL = DH / 4, PP = 64 / FL;
+    const int f4 = lane % FL, pg = lane / FL;
     const float2 x = lane < np ? ml[lane] : make_float2(-INFINITY, 0.f);
     const float mx = wave_max(x.x), f = x.x == mx ? 1.f : __builtin_amdgcn_exp2f(x.x - mx);
     const float sum = wave_sum(x.y * f);
-    constexpr int N = DH < 64 ? 1 : DH / 64;
-    float v[N] = {};
-    if (lane * N < DH)
-        for (int p = 0; p < np; ++p) {
-            const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), p));
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] += w * part[(int64_t)p * DH + lane * N + e];
-        }
-    if (lane * N >= DH) return;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T* out = (T*)a.out + (int64_t)(r0 + i) * a.ldo + (int64_t)head * DH + lane * N;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        if constexpr (sizeof(T) == 2) out[e] = f32_to_bf16(v[e] * inv);
-        else out[e] = v[e] * inv;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = pg; p < np; p += PP) {
+        const float mp = ml[p].x, w = mp == mx ? 1.f : __builtin_amdgcn_exp2f(mp - mx);
+        const float4 y = *(const float4*)(part + (int64_t)p * DH + f4 * 4);
+        v.x += w * y.x; v.y += w * y.y; v.z += w * y.z; v.w += w * y.w;
     }
+#pragma unroll
+    for (int d = FL; d < 64; d <<= 1) {
+        v.x += __shfl_xor(v.x, d, 64);
+        v.y += __shfl_xor(v.y, d, 64);
+        v.z += __shfl_xor(v.z, d, 64);
+        v.w += __shfl_xor(v.w, d, 64);
+    }
+    if (pg == 0)
+        store4<T>((T*)a.out + (int64_t)(r0 + i) * a.ldo + (int64_t)head * DH + f4 * 4, scaled(v, sum == 0.f ? 0.f : 1.f / sum));
 }
 
+// Shapes of a workgroup: wavefronts that share a column tile, column tiles side by side.
+struct AttnShape {
+    int kw, cw;
+};
+static constexpr AttnShape SHAPES[] = {{8, 1}, {4, 1}, {2, 2}, {1, 4}};
+
+// Wavefronts per column tile: as many as leave some six wavefronts per SIMD in all (three of the larger ones of
+// head dimension 128), since a tile's chain of loads, products and exponentials wants others beside it; but where the
+// column tiles alone give every CU work, at least six tiles of tokens each (the first loads and the meeting in
+// LDS cost about as much as two).  Measured, us, with 8 | 4 | 2 | 1: 3072 column tiles of causal prompts over 4096
+// tokens - | 109 | 100 | 105; 2048 tiles of head dimension 128 over 1500 tokens - | 72 | 65 | 61; 768 tiles (64 x 16
+// rows, 12 heads, 4096 tokens) 56 | 56 | 59 | -; 768 tiles over 1024 tokens 21 | 18 | 19 | -; 320 tiles (2 x 300 rows,
+// 16 heads, 900 tokens) 13 | 10 | 12 | 20; 192 tiles (8 x 40 rows, 12 heads, 4096 tokens) 18 | 20 | 22 | 33.
+// Pieces: cutting a sequence costs the partial results' way through memory and a second launch (768 tiles:
+// 56 us whole, 73 in two), so it is done only while the workgroups are fewer than half the CUs, for pieces of 1024
+// tokens and more (1 row, 8 heads, 32768 tokens: 20 us in 16 pieces, 27 in 8; 12 heads, 1001 tokens: 7.1 us whole,
+// 8.2 in four).
 CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int dh, int32_t max_new, int32_t max_kv) {
     CacheAttnPlan p;
-    const int64_t cols = (int64_t)max_new * (Hq / Hkv);
-    p.kw = cols <= 32 ? 4 : cols <= 64 ? 2 : 1;
-    const int64_t wgs = std::max<int64_t>(1, (int64_t)S * Hkv * ceil_div(cols, 32 * (4 / p.kw)));
-    const int64_t want = std::min<int64_t>(64, std::max<int64_t>(1, ceil_div(2048, wgs)));
-    const int64_t unit = 32 * p.kw;
-    const int64_t chunk = std::max<int64_t>(2 * unit, ceil_div(ceil_div(max_kv, want), unit) * unit);
-    p.chunk = (int)std::min<int64_t>(chunk, ceil_div(max_kv, unit) * unit);
+    const int64_t cols = (int64_t)max_new * (Hq / Hkv), per = std::max<int64_t>(1, (int64_t)S * Hkv);
+    const int64_t tiles = std::max<int64_t>(1, per * ceil_div(cols, 32));
+    int64_t waves = (dh > 64 ? 3072 : 6144) / tiles;
+    if (tiles > 256) waves = std::min(waves, ceil_div(max_kv, 32) / 6);
+    p.shape = waves >= 8 ? 0 : waves >= 4 ? 1 : waves >= 2 ? 2 : 3;
+    const AttnShape sh = SHAPES[p.shape];
+    p.tiles = ceil_div(cols, 32 * sh.cw);
+    const int64_t wgs = per * p.tiles;
+    int64_t chunk = ceil_div(max_kv, 32) * 32;
+    if (wgs < 128) chunk = std::min(chunk, std::max<int64_t>(1024, ceil_div(max_kv, ceil_div(256, wgs))));
+    chunk = std::max<int64_t>(ceil_div(chunk, 32) * 32, ceil_div(ceil_div(max_kv, 64), 32) * 32);   // at most 64 pieces
+    p.chunk = (int)chunk;
     p.nsplit = (int)ceil_div(max_kv, p.chunk);
     p.ws = p.nsplit == 1 ? 0 : ((size_t)T * Hq * p.nsplit * (dh + 2) * sizeof(float) + 255) & ~(size_t)255;
     return p;
 }
 
+template <typename T, int DH, int I>
+static void launch_shape(const CacheAttnArgs& a, dim3 grid, hipStream_t s) {
+    constexpr AttnShape h = SHAPES[I];
+    launch_k((cache_attn_kernel<T, DH, h.kw, h.cw, 2>), grid, dim3(64 * h.kw * h.cw), 0, s, a);
+}
+
 template <typename T, int DH>
-static void launch_cache_attn_t(const CacheAttnArgs& a, int kw, hipStream_t s) {
+static void launch_cache_attn_t(const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     const int64_t groups = (int64_t)a.S * a.c.H * a.nsplit;
-    const int64_t tiles = ceil_div((int64_t)a.max_new * a.G, 32 * (4 / kw));
-    const dim3 grid((unsigned)(ceil_div(groups, 8) * 8 * tiles));
+    const dim3 grid((unsigned)(ceil_div(groups, 8) * 8 * p.tiles));
     {
         ProfScope ps(KC_CACHE_ATTN, s);
-        if (kw == 4) launch_k((cache_attn_kernel<T, DH, 4>), grid, dim3(256), 0, s, a);
-        else if (kw == 2) launch_k((cache_attn_kernel<T, DH, 2>), grid, dim3(256), 0, s, a);
-        else launch_k((cache_attn_kernel<T, DH, 1>), grid, dim3(256), 0, s, a);
+        switch (p.shape) {
+            case 0: launch_shape<T, DH, 0>(a, grid, s); break;
+            case 1: launch_shape<T, DH, 1>(a, grid, s); break;
+            case 2: launch_shape<T, DH, 2>(a, grid, s); break;
+            default: launch_shape<T, DH, 3>(a, grid, s); break;
+        }
     }
     if (a.nsplit > 1) {
         ProfScope ps(KC_CACHE_ATTN, s);
@@ -406,12 +481,12 @@ static void launch_cache_attn_t(const CacheAttnArgs& a, int kw, hipStream_t s) {
     }
 }
 
-dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, int kw, hipStream_t s) {
+dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s) {
     switch (a.dh) {
 #define X(d)                                                          \
     case d:                                                           \
-        if (dtype == DD_BF16) launch_cache_attn_t<bf16_t, d>(a, kw, s); \
-        else launch_cache_attn_t<float, d>(a, kw, s);                 \
+        if (dtype == DD_BF16) launch_cache_attn_t<bf16_t, d>(a, p, s); \
+        else launch_cache_attn_t<float, d>(a, p, s);                  \
         break;
         X(32) X(64) X(128)
 #undef X

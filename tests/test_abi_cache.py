@@ -91,7 +91,7 @@ def test_nothing_to_do_is_done():
     (dict(scale=-1.0), 1), (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(max_new=0), 1), (dict(max_kv=0), 1),
     (dict(max_kv=257), 2), (dict(ldq=255), 2), (dict(ldq=260), 2), (dict(ldo=248), 2), (dict(q=None), 1), (dict(out=None), 1),
     (dict(codes=None), 1), (dict(q=FAKE + 2), 1), (dict(out=FAKE + 8), 1), (dict(ws=FAKE, wsb=16), 4), (dict(ws=None, wsb=1 << 40), 1),
-    (dict(ws=FAKE + 64, wsb=1 << 40), 1), (dict(max_new=1 << 30), 6)])
+    (dict(ws=FAKE + 64, wsb=1 << 40), 1), (dict(max_kv=(1 << 30) + 1), 6), (dict(max_new=1 << 30), 6)])
 def test_attention_refusals(kw, status):
     m = _map(ld_table=4 if kw.get("wsb", 0) == 0 else 64)
     if kw.get("wsb", 0):
