@@ -557,7 +557,7 @@ dd_status dd_cache_plan(const dd_cache* cache, const dd_cache_map* map, const in
  * dd_cache_append - keys and values of a pass's rows into the cache.
  *   k, v         device [T] rows of n_kv_heads * dh numbers of `dtype`, head h at h * dh, row stride ld
  *                elements (the packed q | k | v rows of a projection are read in place); 16-byte aligned,
- *                ld * element size a multiple of 16, ld >= n_kv_heads * dh
+ *                ld * element size a multiple of 16, n_kv_heads * dh <= ld <= 2^21
  *   Per block, head and kind (key or value), a the largest finite |x| of the rows that fall into it: the
  *   scale is the smallest 2^e with a <= 448 * 2^e, e clamped to [-100, 120].  A block whose first new token
  *   is not its first place has older tokens: it keeps its scale where that is larger, else takes the new

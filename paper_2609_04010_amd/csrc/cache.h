@@ -49,10 +49,9 @@ struct AppendArgs {
     int32_t dh, S, T;
     uint8_t* codes;
     float* scales;
-    const int32_t *row_start, *row_seq, *slots;
+    const int32_t *kv_len, *row_start, *row_seq, *slots;
     const void *k, *v;
     int64_t ld;
-    int rows_per_wg;   // set by launch_cache_append
     int32_t* err;
 };
 dd_status launch_cache_append(int dtype, const AppendArgs& a, hipStream_t s);

@@ -940,12 +940,15 @@ dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, con
     DD_CHECK(dtype == DD_BF16 || dtype == DD_FP32, DD_E_DTYPE, "unknown dtype");
     DD_CHECK(ld >= (int64_t)cache->n_kv_heads * cache->head_dim && ld * (int64_t)esize(dtype) % 16 == 0, DD_E_SHAPE,
              "ld must be >= n_kv_heads * head_dim and a multiple of 16 bytes");
+    DD_CHECK(ld <= (1 << 21), DD_E_UNSUPPORTED, "ld above 2^21 unsupported");
+    DD_CHECK(((double)map->T / cache->block + 2.0 * map->S) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
+             "too many blocks: T and S are too large");
     if (map->S == 0 || map->T == 0) return DD_OK;
     DD_CHECK(codes && scales && k && v, DD_E_ARG, "NULL pointer argument");
     DD_CHECK((((uintptr_t)codes | (uintptr_t)k | (uintptr_t)v) & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
              "codes, k and v must be 16-byte aligned, scales 8-byte aligned");
-    AppendArgs a = {cache_shape(cache), cache->head_dim, map->S, map->T, (uint8_t*)codes, scales, map->row_start,
-                    map->row_seq, map->slots, k, v, ld, 0, dev_err};
+    AppendArgs a = {cache_shape(cache), cache->head_dim, map->S, map->T, (uint8_t*)codes, scales, map->kv_len,
+                    map->row_start, map->row_seq, map->slots, k, v, ld, dev_err};
     return launch_cache_append(dtype, a, (hipStream_t)stream);
 }
 

@@ -229,34 +229,43 @@ dd_status launch_cache_plan(const PlanArgs& a, hipStream_t s) {
 
 // ---------------------------------------------------------------- append
 //
-// A unit of work is one (block, head, keys or values) that a sequence's rows fall into: the workgroup
-// takes the largest finite |x| of its rows (at most P dh numbers), fixes the scale from its exponent and
-// mantissa bits, and writes the codes.  The unit's first row (the "leader": the first place of a block,
-// or the sequence's first row) stands for it; a workgroup looks for leaders among rows_per_wg rows and
-// does their units in turn.  Each of its four wavefronts owns slabs of 32 tokens, held in registers
-// between the maximum and the codes, so the rows are read once.
+// A unit of work is one (block, head, keys or values) that a sequence's rows fall into: take the largest finite
+// |x| of its rows (at most P dh numbers), fix the scale from its exponent and mantissa bits, write the codes.
+// Sequence s touches ceil((o_s + n_s) / P) blocks, o_s the place of its first new token; a wavefront finds its
+// unit by a prefix sum of those over the lanes, 64 sequences at a time, so the grid has about as many
+// units as there are (T / P + 2 S at most) and hardly a workgroup without work.
+//
+// Slabs of 32 tokens stay in registers between the maximum and the codes, so the rows are read once; W
+// wavefronts share a unit's slabs: one where sequences add few tokens (then the four wavefronts of a workgroup
+// have units of their own and nothing waits at a barrier), four for prompts.
 //
 // Keys: a lane holds 8 features of a token (16-byte loads of bf16) and stores 8 codes.  Values: a lane
 // holds 2 features of TPL tokens that are neighbours in the cache's [dh][32] slab and stores TPL codes at
 // a time; a slab whose places are not all new is read, changed and written back in the same lanes.
 
-template <typename T> DD_DEV void load8(const T* p, float (&x)[8]);
-template <> DD_DEV void load8<bf16_t>(const bf16_t* p, float (&x)[8]) {
-    const uint4 u = *(const uint4*)p;
-    x[0] = bf16_lo(u.x); x[1] = bf16_hi(u.x); x[2] = bf16_lo(u.y); x[3] = bf16_hi(u.y);
-    x[4] = bf16_lo(u.z); x[5] = bf16_hi(u.z); x[6] = bf16_lo(u.w); x[7] = bf16_hi(u.w);
-}
-template <> DD_DEV void load8<float>(const float* p, float (&x)[8]) {
-    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-template <typename T> DD_DEV float2 load2(const T* p);
-template <> DD_DEV float2 load2<bf16_t>(const bf16_t* p) {
-    const uint32_t u = *(const uint32_t*)p;
-    return make_float2(bf16_lo(u), bf16_hi(u));
-}
-template <> DD_DEV float2 load2<float>(const float* p) { return *(const float2*)p; }
+// N neighbouring numbers of a row as they stand in memory, and one of them as fp32
+template <typename T, int N> struct Raw {
+    uint32_t w[N * sizeof(T) / 4];
+    DD_DEV void load(const T* p) {
+        constexpr int W = N * sizeof(T) / 4;
+        if constexpr (W == 1) {
+            w[0] = *(const uint32_t*)p;
+        } else if constexpr (W == 2) {
+            const uint2 u = *(const uint2*)p;
+            w[0] = u.x; w[1] = u.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; i += 4) {
+                const uint4 u = *(const uint4*)((const uint32_t*)p + i);
+                w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
+            }
+        }
+    }
+    DD_DEV float operator[](int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return e & 1 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+    }
+};
 
 // largest |x| over finite x, as bits (of non-negative floats, which order like their bits)
 DD_DEV uint32_t amax_bits(uint32_t m, float x) {
@@ -277,11 +286,14 @@ DD_DEV uint32_t rescale4(uint32_t c, float f) {
     return enc_fp8x4(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
 }
 
-// One unit: rows r .. r + n - 1 at places off .. off + n - 1 of the block whose codes (keys or values) start
-// at `body` and whose scale is *scale.
-template <typename T, int DH, bool VALUES>
-DD_DEV void append_unit(const T* x, int64_t ld, int n, int off, int P, uint8_t* body, float* scale, uint32_t* red) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+// the lowest n bytes (none for n <= 0, all for n >= 4)
+DD_DEV uint32_t low_bytes(int n) { return n <= 0 ? 0u : 0xFFFFFFFFu >> (32 - 8 * min(n, 4)); }
+
+// One unit: n rows from x on at places off .. off + n - 1 of the block whose codes (keys or values) start at
+// `body` and whose scale is *scale, by W wavefronts of which this is number w.
+template <typename T, int DH, bool VALUES, int W>
+DD_DEV void append_unit(const T* x, int64_t ld, int n, int off, int P, uint8_t* body, float* scale, int w, uint32_t* red) {
+    const int lane = threadIdx.x & 63;
     constexpr int LPT = VALUES ? DH / 2 : DH / 8;        // lanes per token
     constexpr int TG = 64 / LPT;                         // tokens side by side
     constexpr int TPL = 32 / TG;                         // tokens of a slab per lane
@@ -289,37 +301,59 @@ DD_DEV void append_unit(const T* x, int64_t ld, int n, int off, int P, uint8_t* 
     const int f = lane % LPT * NF, tg = lane / LPT;
     // token of the slab: keys TG apart (a store covers whole rows), values neighbours
     auto tok = [&](int i) { return VALUES ? tg * TPL + i : i * TG + tg; };
-    const int end = off + n;
-    float v[2][TPL][NF] = {};   // P <= 256: at most two slabs per wavefront
-    uint32_t m = 0;
+    const int end = off + n, first = off >> 5, slabs = ((end + 31) >> 5) - first;   // the slabs with new places
+    const float s_old = off > 0 ? *scale : 0.f;
+    const uint32_t ldb = (uint32_t)ld * sizeof(T);   // (256 rows of at most 2^21 numbers: below 2^32)
+    Raw<T, NF> v[2][TPL];
+    uint32_t old[2][2][TPL / 4];   // values: the codes that stand where this lane will write
+    // All loads of two slabs at once; places that are not new take a neighbouring row, which changes no maximum and
+    // is not stored.
+    auto load = [&](int j0) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int t0 = (w + 4 * j) * 32;
-        if (t0 >= end || t0 + 32 <= off) continue;
+        for (int j = 0; j < 2; ++j) {
+            const int sl = j0 + w + W * j, t0 = (first + sl) * 32;
+            if (sl >= slabs) continue;
 #pragma unroll
-        for (int i = 0; i < TPL; ++i) {
-            const int t = t0 + tok(i);
-            if (t >= off && t < end) {
-                const T* p = x + (int64_t)(t - off) * ld + f;
-                if constexpr (VALUES) {
-                    const float2 y = load2<T>(p);
-                    v[j][i][0] = y.x;
-                    v[j][i][1] = y.y;
-                } else {
-                    load8<T>(p, v[j][i]);
+            for (int i = 0; i < TPL; ++i) v[j][i].load((const T*)((const char*)x + (uint32_t)(min(max(t0 + tok(i), off), end - 1) - off) * ldb) + f);
+            if (VALUES && (t0 < off || t0 + 32 > end)) {
+#pragma unroll
+                for (int e2 = 0; e2 < 2; ++e2) {
+                    const uint32_t* p = (const uint32_t*)(body + (int64_t)t0 * DH + (f + e2) * 32 + tg * TPL);
+                    if constexpr (TPL == 8) {
+                        const uint2 u = *(const uint2*)p;
+                        old[j][e2][0] = u.x; old[j][e2][1] = u.y;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < TPL / 16; ++i) {
+                            const uint4 u = ((const uint4*)p)[i];
+                            old[j][e2][4 * i] = u.x; old[j][e2][4 * i + 1] = u.y;
+                            old[j][e2][4 * i + 2] = u.z; old[j][e2][4 * i + 3] = u.w;
+                        }
+                    }
                 }
             }
+        }
+    };
+    uint32_t m = 0;
+    for (int j0 = 0; j0 < slabs; j0 += 2 * W) {
+        load(j0);
 #pragma unroll
-            for (int e = 0; e < NF; ++e) m = amax_bits(m, v[j][i][e]);
+        for (int j = 0; j < 2; ++j) {
+            if (j0 + w + W * j >= slabs) continue;
+#pragma unroll
+            for (int i = 0; i < TPL; ++i)
+#pragma unroll
+                for (int e = 0; e < NF; ++e) m = amax_bits(m, v[j][i][e]);
         }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-    __syncthreads();   // the last unit's readers are done with red and with *scale
-    if (lane == 0) red[w] = m;
-    const float s_old = off > 0 ? *scale : 0.f;
-    __syncthreads();
-    m = max(max(red[0], red[1]), max(red[2], red[3]));
+    if constexpr (W > 1) {
+        if (lane == 0) red[w] = m;
+        __syncthreads();   // (also: every wavefront has read *scale)
+#pragma unroll
+        for (int i = 0; i < W; ++i) m = max(m, red[i]);
+    }
     int e = scale_exp(m);
     float again = 1.f;   // what the block's other codes are multiplied by
     if (off > 0) {
@@ -327,120 +361,175 @@ DD_DEV void append_unit(const T* x, int64_t ld, int n, int off, int P, uint8_t* 
         if (e > eo) again = pow2i(max(eo - e, -126));
         e = max(e, eo);
     }
-    if (threadIdx.x == 0) *scale = pow2i(e);
+    if (w == 0 && lane == 0) *scale = pow2i(e);
     const float inv = pow2i(-e);
+    auto encode = [&](int j0) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int t0 = (w + 4 * j) * 32;
-        const bool fresh = t0 < end && t0 + 32 > off;    // has new places
-        if (t0 >= P || (!fresh && again == 1.f)) continue;
-        if constexpr (!VALUES) {
+        for (int j = 0; j < 2; ++j) {
+            const int sl = j0 + w + W * j, t0 = (first + sl) * 32;
+            if (sl >= slabs) continue;
+            if constexpr (!VALUES) {
 #pragma unroll
-            for (int i = 0; i < TPL; ++i) {
-                const int t = t0 + tok(i);
-                uint2* p = (uint2*)(body + (int64_t)t * DH + f);
-                if (t >= off && t < end) {
-                    const auto& y = v[j][i];
-                    *p = make_uint2(enc_fp8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                                    enc_fp8x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
-                } else if (again != 1.f) {
-                    const uint2 c = *p;
-                    *p = make_uint2(rescale4(c.x, again), rescale4(c.y, again));
+                for (int i = 0; i < TPL; ++i) {
+                    const int t = t0 + tok(i);
+                    uint2* p = (uint2*)(body + (int64_t)t * DH + f);
+                    if (t >= off && t < end) {
+                        const auto& y = v[j][i];
+                        *p = make_uint2(enc_fp8x4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
+                                        enc_fp8x4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+                    } else if (again != 1.f) {
+                        const uint2 c = *p;
+                        *p = make_uint2(rescale4(c.x, again), rescale4(c.y, again));
+                    }
                 }
-            }
-        } else {
-            const int a0 = t0 + tg * TPL;                // this lane's first token
-            const bool whole = a0 >= off && a0 + TPL <= end;
+            } else {
+                const int a0 = t0 + tg * TPL;                // this lane's first token
+                const bool whole = a0 >= off && a0 + TPL <= end;
+                if (again == 1.f && (a0 + TPL <= off || a0 >= end)) continue;
 #pragma unroll
-            for (int e2 = 0; e2 < 2; ++e2) {
-                uint32_t* p = (uint32_t*)(body + (int64_t)t0 * DH + (f + e2) * 32 + tg * TPL);
-                uint32_t c[TPL / 4];
-                if (!whole) {
+                for (int e2 = 0; e2 < 2; ++e2) {
+                    uint32_t* p = (uint32_t*)(body + (int64_t)t0 * DH + (f + e2) * 32 + tg * TPL);
+                    uint32_t c[TPL / 4];
+#pragma unroll
+                    for (int i = 0; i < TPL / 4; ++i) {
+                        const uint32_t nw = enc_fp8x4(v[j][4 * i][e2] * inv, v[j][4 * i + 1][e2] * inv,
+                                                      v[j][4 * i + 2][e2] * inv, v[j][4 * i + 3][e2] * inv);
+                        if (whole) {
+                            c[i] = nw;
+                        } else {
+                            const uint32_t od = again != 1.f ? rescale4(old[j][e2][i], again) : old[j][e2][i];
+                            const uint32_t in = low_bytes(end - (a0 + 4 * i)) & ~low_bytes(off - (a0 + 4 * i));
+                            c[i] = (nw & in) | (od & ~in);
+                        }
+                    }
                     if constexpr (TPL == 8) {
-                        const uint2 u = *(const uint2*)p;
-                        c[0] = u.x; c[1] = u.y;
+                        *(uint2*)p = make_uint2(c[0], c[1]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < TPL / 16; ++i) {
-                            const uint4 u = ((const uint4*)p)[i];
-                            c[4 * i] = u.x; c[4 * i + 1] = u.y; c[4 * i + 2] = u.z; c[4 * i + 3] = u.w;
-                        }
+                        for (int i = 0; i < TPL / 16; ++i)
+                            ((uint4*)p)[i] = make_uint4(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
                     }
-                }
-#pragma unroll
-                for (int i = 0; i < TPL / 4; ++i) {
-                    const uint32_t nw = enc_fp8x4(v[j][4 * i][e2] * inv, v[j][4 * i + 1][e2] * inv,
-                                                  v[j][4 * i + 2][e2] * inv, v[j][4 * i + 3][e2] * inv);
-                    if (whole) {
-                        c[i] = nw;
-                    } else {
-                        const uint32_t od = again != 1.f ? rescale4(c[i], again) : c[i];
-                        uint32_t y = 0;
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            const int t = a0 + 4 * i + b;
-                            y |= (t >= off && t < end ? nw : od) & (0xFFu << (8 * b));
-                        }
-                        c[i] = y;
-                    }
-                }
-                if constexpr (TPL == 8) {
-                    *(uint2*)p = make_uint2(c[0], c[1]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < TPL / 16; ++i)
-                        ((uint4*)p)[i] = make_uint4(c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]);
                 }
             }
         }
+    };
+    if (slabs <= 2 * W) {
+        encode(0);
+    } else {
+        for (int j0 = 0; j0 < slabs; j0 += 2 * W) {
+            load(j0);
+            encode(j0);
+        }
     }
+    if (again != 1.f)   // slabs without new places
+        for (int sl = w; sl < P >> 5; sl += W)
+            if (sl < first || sl >= first + slabs)
+                for (int i = lane; i < 2 * DH; i += 64) {
+                    uint4* p = (uint4*)(body + (int64_t)sl * 32 * DH) + i;
+                    const uint4 c = *p;
+                    *p = make_uint4(rescale4(c.x, again), rescale4(c.y, again), rescale4(c.z, again), rescale4(c.w, again));
+                }
 }
 
-template <typename T, int DH>
+// Wavefront sum of whole numbers (the lane moves of wave_sum_dpp).
+template <int CTRL, int ROWS> DD_DEV int dpp_add_int(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+DD_DEV int wave_sum_int(int v) {
+    v = dpp_add_int<0xB1, 0xF>(v);
+    v = dpp_add_int<0x4E, 0xF>(v);
+    v = dpp_add_int<0x141, 0xF>(v);
+    v = dpp_add_int<0x140, 0xF>(v);
+    v = dpp_add_int<0x142, 0xA>(v);
+    v = dpp_add_int<0x143, 0xC>(v);
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The u-th touched block of the pass: its sequence and which of the sequence's touched blocks it is.  false: there
+// are not so many.  256 sequences' loads at a time; only the 64 that u falls into are scanned.
+DD_DEV bool append_find(const AppendArgs& a, int u, int lane, int& seq, int& j, int& off, int& r0, int& n) {
+    for (int s0 = 0; s0 < a.S; s0 += 256) {
+        int b[4], e[4], o[4], nb[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int s = min(s0 + 64 * c + lane, a.S - 1);
+            b[c] = a.row_start[s];
+            e[c] = a.row_start[s + 1];
+            o[c] = a.kv_len[s];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            b[c] = min(max(b[c], 0), a.T);
+            e[c] = min(max(e[c], b[c]), a.T);
+            o[c] = (o[c] - (e[c] - b[c])) & (a.c.P - 1);
+            nb[c] = e[c] > b[c] && s0 + 64 * c + lane < a.S ? (o[c] + (e[c] - b[c]) + a.c.P - 1) >> a.c.log2p : 0;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int total = wave_sum_int(nb[c]);
+            if (u < total) {
+                int inc = nb[c];
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int up = __shfl_up(inc, d, 64);
+                    if (lane >= d) inc += up;
+                }
+                const int at = __popcll(__ballot(inc <= u));   // the first lane whose sum passes u
+                seq = s0 + 64 * c + at;
+                j = u - (__builtin_amdgcn_readlane(inc, at) - __builtin_amdgcn_readlane(nb[c], at));
+                off = __builtin_amdgcn_readlane(o[c], at);
+                r0 = __builtin_amdgcn_readlane(b[c], at);
+                n = __builtin_amdgcn_readlane(e[c], at) - r0;
+                return true;
+            }
+            u -= total;
+        }
+    }
+    return false;
+}
+
+template <typename T, int DH, int W>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     __shared__ uint32_t red[4];
-    const int lane = threadIdx.x & 63;
-    const int h = blockIdx.y >> 1, values = blockIdx.y & 1;
-    const int r0 = blockIdx.x * a.rows_per_wg;
-    // lane i looks at row r0 + i: its slot, and how many rows of its block it leads (0: none)
-    int slot = -1, n = 0;
-    if (lane < a.rows_per_wg && r0 + lane < a.T) {
-        const int r = r0 + lane;
-        slot = a.slots[r];
-        const int s = a.row_seq[r];
-        if (slot >= 0 && s >= 0 && s < a.S && slot < a.c.n_blocks * a.c.P) {
-            const int off = slot & (a.c.P - 1);
-            if (off == 0 || r == a.row_start[s]) n = min(min(a.row_start[s + 1], a.T) - r, a.c.P - off);
-        } else if ((slot >= 0 || s >= 0) && a.err && blockIdx.y == 0 && threadIdx.x < 64) {
-            atomicOr(a.err, DD_DEVERR_CACHE);
-        }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // head and kind run fastest: workgroups that run together read whole rows
+    const int per = W == 4 ? 2 * a.c.H : (2 * a.c.H + 3) / 4, unit = blockIdx.x / per;
+    const int hk = W == 4 ? blockIdx.x - unit * per : (blockIdx.x - unit * per) * 4 + wave;
+    if (W == 1 && hk >= 2 * a.c.H) return;
+    const int values = hk >= a.c.H, h = values ? hk - a.c.H : hk;
+    int seq, j, off, r, n;
+    if (!append_find(a, unit, lane, seq, j, off, r, n)) return;
+    // rows and places of the sequence's j-th touched block
+    if (j > 0) {
+        const int skip = (j << a.c.log2p) - off;
+        r += skip;
+        n -= skip;
+        off = 0;
     }
-    uint64_t todo = __ballot(n > 0);
-    while (todo) {
-        const int i = __ffsll((unsigned long long)todo) - 1;
-        todo &= todo - 1;
-        const int sl = __builtin_amdgcn_readlane(slot, i), cnt = __builtin_amdgcn_readlane(n, i);
-        const int64_t block = sl >> a.c.log2p;
-        uint8_t* body = a.codes + cache_slab(a.c, DH, block, h) + (values ? (int64_t)a.c.P * DH : 0);
-        float* scale = a.scales + (block * a.c.H + h) * 2 + values;
-        const T* x = (const T*)(values ? a.v : a.k) + (int64_t)(r0 + i) * a.ld + (int64_t)h * DH;
-        if (values) append_unit<T, DH, true>(x, a.ld, cnt, sl & (a.c.P - 1), a.c.P, body, scale, red);
-        else append_unit<T, DH, false>(x, a.ld, cnt, sl & (a.c.P - 1), a.c.P, body, scale, red);
+    n = min(n, a.c.P - off);
+    const int slot = a.slots[r];
+    if (slot < 0 || slot >= a.c.n_blocks * a.c.P || (slot & (a.c.P - 1)) != off || a.row_seq[r] != seq) {
+        if (a.err && threadIdx.x == 0) atomicOr(a.err, DD_DEVERR_CACHE);
+        return;
     }
+    const int64_t block = slot >> a.c.log2p;
+    uint8_t* body = a.codes + cache_slab(a.c, DH, block, h) + (values ? (int64_t)a.c.P * DH : 0);
+    float* scale = a.scales + (block * a.c.H + h) * 2 + values;
+    const T* x = (const T*)(values ? a.v : a.k) + (int64_t)r * a.ld + (int64_t)h * DH;
+    const int w = W == 4 ? wave : 0;
+    if (values) append_unit<T, DH, true, W>(x, a.ld, n, off, a.c.P, body, scale, w, red);
+    else append_unit<T, DH, false, W>(x, a.ld, n, off, a.c.P, body, scale, w, red);
 }
 
-dd_status launch_cache_append(int dtype, const AppendArgs& args, hipStream_t s) {
-    AppendArgs a = args;
-    // rows per workgroup: enough workgroups to fill the CUs twice over with units of few rows, no more
-    // than 32 rows (the smallest block) so that prompts spread over all units
-    const int64_t units = (int64_t)a.T * 2 * a.c.H;
-    a.rows_per_wg = (int)std::min<int64_t>(32, std::max<int64_t>(1, units / 4096));
+dd_status launch_cache_append(int dtype, const AppendArgs& a, hipStream_t s) {
     ProfScope ps(KC_CACHE_APPEND, s);
-    const dim3 grid((unsigned)ceil_div(a.T, a.rows_per_wg), 2 * a.c.H);
-#define X(T, d)                                                                    \
-    if (a.dh == d) {                                                               \
-        launch_k((cache_append_kernel<T, d>), grid, dim3(256), 0, s, a);           \
-        return launch_status("cache_append");                                      \
+    const int64_t units = std::min<int64_t>(a.T, a.T / a.c.P + 2 * (int64_t)a.S);
+    // sequences that add 32 rows or more on average: four wavefronts per unit
+    const bool wide = a.T >= 32 * (int64_t)a.S;
+    const dim3 grid((unsigned)(units * (wide ? 2 * a.c.H : (2 * a.c.H + 3) / 4)));
+#define X(T, d)                                                                          \
+    if (a.dh == d) {                                                                     \
+        if (wide) launch_k((cache_append_kernel<T, d, 4>), grid, dim3(256), 0, s, a);    \
+        else launch_k((cache_append_kernel<T, d, 1>), grid, dim3(256), 0, s, a);         \
+        return launch_status("cache_append");                                            \
     }
     if (dtype == DD_BF16) { X(bf16_t, 32) X(bf16_t, 64) X(bf16_t, 128) }
     else { X(float, 32) X(float, 64) X(float, 128) }

@@ -73,7 +73,7 @@ def test_plan_refuses_null(name):
     assert _plan(None, _map()) == 1 and _plan(_cache(), None) == 1
 
 
-@pytest.mark.parametrize("kw,status", [(dict(dtype=2), 3), (dict(ld=127), 2), (dict(ld=132), 2), (dict(ld=126, dtype=1), 2),
+@pytest.mark.parametrize("kw,status", [(dict(dtype=2), 3), (dict(ld=(1 << 21) + 8), 6), (dict(ld=127), 2), (dict(ld=132), 2), (dict(ld=126, dtype=1), 2),
                                        (dict(codes=None), 1), (dict(scales=None), 1), (dict(k=None), 1), (dict(v=None), 1),
                                        (dict(k=FAKE + 8), 1), (dict(codes=FAKE + 4), 1), (dict(scales=FAKE + 4), 1)])
 def test_append_refusals(kw, status):
