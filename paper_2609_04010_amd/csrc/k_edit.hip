@@ -1,10 +1,16 @@
 // Penalties for repeated tokens, biases and allowed-token masks on rows of logits.
 //
-// A workgroup owns a piece of EC classes and walks rows_per_wg rows: the counts of the history's tokens and
-// the biases of its classes stand in LDS (whole numbers, so the order of the atomics does not show), and each
-// row's piece is read, edited and written in one pass.  Rows of one sequence share their counts: a longer
-// history adds its new entries, a shorter one (or another sequence) begins again.  Bound by the memory
-// traffic of the logits.
+// A workgroup owns a piece of EC classes and walks rows_per_wg rows, R at a time.  In LDS stand the counts of the
+// history's tokens and the biases of its classes, and a list of the classes that have either (whole numbers, so the
+// order of the atomics does not show).  The rows' pieces pass through LDS as they are in memory: there the listed
+// classes are edited, one per thread whatever rows they belong to, and every thread takes its 16 bytes back,
+// applies the mask to the packed numbers and stores them.  Rows of one sequence share their counts: a longer history adds its new entries, a shorter one (or another
+// sequence) begins again.
+//
+// Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.60 ms with any one kind of edit and
+// 0.76 ms with all (a copy 0.67 ms), 4.3 TB/s.  Of 1024, 2048 and 4096 classes and 2, 4 and 8 rows the one here was
+// fastest (0.81 to 1.03 ms).  Every global load of the R rows is on its way before one is waited for: a wait for a
+// row's mask number between them cost 0.3 ms.
 #include <math.h>
 
 #include <algorithm>
@@ -14,119 +20,198 @@
 
 namespace dd {
 
-constexpr int EC = 4096;   // classes of a workgroup: 32 KB of LDS, five workgroups per CU
+constexpr int EC = 2048;   // classes of a workgroup
 constexpr int ET = 256;
 
-template <typename T> DD_DEV void store_chunk(T* p, const float (&x)[Elem<T>::E]);
-template <> DD_DEV void store_chunk<bf16_t>(bf16_t* p, const float (&x)[8]) {
-    *(uint4*)p = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
-template <> DD_DEV void store_chunk<float>(float* p, const float (&x)[4]) { *(float4*)p = make_float4(x[0], x[1], x[2], x[3]); }
 template <typename T> DD_DEV void store_one(T* p, float x);
 template <> DD_DEV void store_one<bf16_t>(bf16_t* p, float x) { *p = f32_to_bf16(x); }
 template <> DD_DEV void store_one<float>(float* p, float x) { *p = x; }
 
-template <typename T>
+// -inf where a bit of ok is clear
+template <typename T> DD_DEV void mask_chunk(uint4& u, uint32_t ok) {
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t keep;
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t lo = (uint32_t)((int32_t)(ok << (31 - 2 * k)) >> 31), hi = (uint32_t)((int32_t)(ok << (30 - 2 * k)) >> 31);
+            keep = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+            w[k] = (w[k] & keep) | (0xFF80FF80u & ~keep);
+        } else {
+            keep = (uint32_t)((int32_t)(ok << (31 - k)) >> 31);
+            w[k] = (w[k] & keep) | (0xFF800000u & ~keep);
+        }
+    }
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// R: rows at a time
+template <typename T, int R>
 __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
-    constexpr int E = Elem<T>::E;
-    __shared__ __attribute__((aligned(16))) uint32_t count[EC];   // how often the class stands in the history
-    __shared__ __attribute__((aligned(16))) uint32_t bias[EC];    // 1 + the last entry of the bias list that names it
+    constexpr int E = Elem<T>::E, NC = EC / (ET * E);   // chunks per thread and row
+    __shared__ __attribute__((aligned(16))) T piece[R][EC];
+    __shared__ __attribute__((aligned(16))) uint32_t count[EC];     // how often the class stands in the history
+    __shared__ __attribute__((aligned(16))) uint32_t bias[EC];      // its bias (while they are gathered: 1 + the last entry
+                                                                    // of the bias list that names it)
+    __shared__ uint32_t some[EC / 32];                              // classes with either,
+    __shared__ uint16_t list[EC];                                   // and the same as a list
+    __shared__ int listed;
     const int tid = threadIdx.x;
     const int v0 = blockIdx.x * EC, nv = min(EC, a.V - v0);
     const int m0 = blockIdx.y * a.rows_per_wg, m1 = min(m0 + a.rows_per_wg, a.rows);
-    const bool hist = a.e.history || a.e.hist_len, biased = a.e.bias_ids != nullptr && a.e.n_bias > 0;
+    const bool biased = a.e.bias_ids != nullptr && a.e.n_bias > 0;
+    const bool lists = a.e.ld_history > 0 || biased;   // some class may need its logit changed
     int seq = -1, have = 0;   // sequence whose tables stand in LDS, entries counted
-    float rep = 1.f, pres = 0.f, freq = 0.f;
-    for (int m = m0; m < m1; ++m) {
-        const int s = m / a.per;
-        int len = 0;
-        if (hist) {
-            const int64_t n = a.e.hist_len ? a.e.hist_len[m] : a.e.ld_history;
-            len = (int)(n < a.e.ld_history ? n : a.e.ld_history);
-        }
-        const bool pass = len < 0;   // the row goes through as it is
-        if (!pass && (s != seq || len < have)) {
-            __syncthreads();         // the last row's readers
-            for (int i = tid; i < EC / 4; i += ET) {
-                ((uint4*)count)[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (s != seq) ((uint4*)bias)[i] = make_uint4(0u, 0u, 0u, 0u);
-            }
-            __syncthreads();
-            if (s != seq && biased)
-                for (int i = tid; i < a.e.n_bias; i += ET) {
-                    const uint32_t v = (uint32_t)a.e.bias_ids[(int64_t)s * a.e.n_bias + i] - (uint32_t)v0;
-                    if (v < (uint32_t)nv) atomicMax(&bias[v], (uint32_t)i + 1u);
-                }
-            if (s != seq) {
-                rep = a.e.repetition ? a.e.repetition[s] : 1.f;
-                pres = a.e.presence ? a.e.presence[s] : 0.f;
-                freq = a.e.frequency ? a.e.frequency[s] : 0.f;
-            }
-            seq = s;
-            have = 0;
-            if (len == 0) __syncthreads();
-        }
-        if (!pass && len > have) {
-            __syncthreads();
-            for (int i = have + tid; i < len; i += ET) {
-                const uint32_t v = (uint32_t)a.e.history[(int64_t)s * a.e.ld_history + i] - (uint32_t)v0;
-                if (v < (uint32_t)nv) atomicAdd(&count[v], 1u);
-            }
-            have = len;
-            __syncthreads();
-        }
-        const uint32_t* allow = nullptr;
-        if (!pass && a.e.allow) {
-            const int id = a.e.allow_id ? a.e.allow_id[m] : 0;
-            if (id >= 0 && id < a.e.n_allow) allow = a.e.allow + (int64_t)id * a.e.ld_allow;
-            else if (id != -1 && a.err && tid == 0 && blockIdx.x == 0) atomicOr(a.err, DD_DEVERR_MASK);
-        }
-        const T* in = (const T*)a.logits + (int64_t)m * a.ld + v0;
-        T* out = (T*)a.out + (int64_t)m * a.ld + v0;
-        for (int c = tid * E; c < nv; c += ET * E) {
-            const uint4 u = *(const uint4*)(in + c);   // ld is a multiple of 8: in bounds
-            float x[E];
+    float rep = 1.f, irep = 1.f, pres = 0.f, freq = 0.f;
+    auto length = [&](int m) {   // history entries of a row; negative: the row goes through as it is
+        const int64_t n = a.e.hist_len ? a.e.hist_len[m] : a.e.ld_history;
+        return (int)(n < a.e.ld_history ? n : a.e.ld_history);
+    };
+    auto add = [&](uint32_t v) {   // class v of this piece into the list
+        const uint32_t bit = 1u << (v & 31u);
+        if (!(atomicOr(&some[v >> 5], bit) & bit)) list[atomicAdd(&listed, 1)] = (uint16_t)v;
+    };
+    for (int g = m0; g < m1; g += R) {
+        const int nr = min(R, m1 - g);
+        uint4 u[R][NC];
+        uint32_t ok[R][NC];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = Elem<T>::get(u, e);
-            if (!pass) {
-                uint32_t n[E], b[E];
+        for (int r = 0; r < R; ++r) {
+            const T* in = (const T*)a.logits + (int64_t)min(g + r, m1 - 1) * a.ld + v0;   // (no branch between the loads)
 #pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const uint4 k = *(const uint4*)&count[c + e], w = *(const uint4*)&bias[c + e];
-                    n[e] = k.x; n[e + 1] = k.y; n[e + 2] = k.z; n[e + 3] = k.w;
-                    b[e] = w.x; b[e + 1] = w.y; b[e + 2] = w.z; b[e + 3] = w.w;
-                }
-                uint32_t ok = 0xFFu;
-                if (allow) ok = allow[(v0 + c) >> 5] >> ((v0 + c) & 31);
+            for (int k = 0; k < NC; ++k)   // (ld is a multiple of 8: in bounds)
+                u[r][k] = *(const uint4*)(in + min((k * ET + tid) * E, (nv - 1) & ~(E - 1)));
+        }
+        if (a.e.allow) {
+            int id[R], len[R];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (n[e]) x[e] = (x[e] > 0.f ? x[e] / rep : x[e] * rep) - (pres + (float)n[e] * freq);
-                    if (b[e]) x[e] += a.e.bias_values[(int64_t)s * a.e.n_bias + (b[e] - 1u)];
-                    if (!(ok >> e & 1u)) x[e] = -INFINITY;
+            for (int r = 0; r < R; ++r) {   // all of them on the way before one is looked at
+                const int m = min(g + r, m1 - 1);
+                id[r] = a.e.allow_id ? a.e.allow_id[m] : 0;
+                len[r] = a.e.hist_len ? a.e.hist_len[m] : 0;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool in = id[r] >= 0 && id[r] < a.e.n_allow, every = !in || len[r] < 0;
+                if (!in && id[r] != -1 && len[r] >= 0 && a.err && tid == 0 && blockIdx.x == 0) atomicOr(a.err, DD_DEVERR_MASK);
+                const uint32_t* allow = a.e.allow + (in ? (int64_t)id[r] * a.e.ld_allow : 0);
+#pragma unroll
+                for (int k = 0; k < NC; ++k) {
+                    const int v = v0 + min((k * ET + tid) * E, (nv - 1) & ~(E - 1));
+                    ok[r][k] = (allow[v >> 5] | (every ? 0xFFFFFFFFu : 0u)) >> (v & 31);
                 }
             }
-            if (c + E <= nv) {
-                store_chunk<T>(out + c, x);
-            } else {
+        }
+        if (lists) {
+            // rows r .. q - 1 at a time that have the same history
+            for (int r = 0; r < nr;) {
+                const int s = (g + r) / a.per, n = length(g + r);
+                int q = r + 1;
+                while (q < nr && (g + q) / a.per == s && length(g + q) == n) ++q;
+                if (n >= 0 && (s != seq || n < have)) {
+                    __syncthreads();         // the last rows' edits
+                    for (int i = tid; i < EC / 4; i += ET) {
+                        ((uint4*)count)[i] = make_uint4(0u, 0u, 0u, 0u);
+                        ((uint4*)bias)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    if (tid < EC / 32) some[tid] = 0u;
+                    if (tid == 0) listed = 0;
+                    __syncthreads();
+                    if (biased) {
+                        for (int i = tid; i < a.e.n_bias; i += ET) {
+                            const uint32_t v = (uint32_t)a.e.bias_ids[(int64_t)s * a.e.n_bias + i] - (uint32_t)v0;
+                            if (v < (uint32_t)nv) {
+                                atomicMax(&bias[v], (uint32_t)i + 1u);
+                                add(v);
+                            }
+                        }
+                        __syncthreads();
+                        for (int i = tid, e = listed; i < e; i += ET) {
+                            const int c = list[i];
+                            bias[c] = __float_as_uint(a.e.bias_values[(int64_t)s * a.e.n_bias + (bias[c] - 1u)]);
+                        }
+                    }
+                    rep = a.e.repetition ? a.e.repetition[s] : 1.f;
+                    irep = 1.f / rep;
+                    pres = a.e.presence ? a.e.presence[s] : 0.f;
+                    freq = a.e.frequency ? a.e.frequency[s] : 0.f;
+                    seq = s;
+                    have = 0;
+                }
+                if (n > have) {
+                    __syncthreads();         // the last rows' edits, the biases
+                    for (int i = have + tid; i < n; i += ET) {
+                        const uint32_t v = (uint32_t)a.e.history[(int64_t)s * a.e.ld_history + i] - (uint32_t)v0;
+                        if (v < (uint32_t)nv) {
+                            atomicAdd(&count[v], 1u);
+                            add(v);
+                        }
+                    }
+                    have = n;
+                }
+                if (r == 0) {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (c + e < nv) store_one<T>(out + c + e, x[e]);
+                    for (int i = 0; i < R; ++i)
+#pragma unroll
+                        for (int k = 0; k < NC; ++k) *(uint4*)&piece[i][(k * ET + tid) * E] = u[i][k];
+                }
+                __syncthreads();
+                const int nl = n >= 0 ? listed : 0;
+                for (int i = tid; i < nl * (q - r); i += ET) {
+                    const int x = i / nl, c = list[i - x * nl];
+                    T* p = &piece[r + x][c];
+                    float y = Elem<T>::load1(p, 0);
+                    const uint32_t k = count[c];
+                    if (k) y = y * (y > 0.f ? irep : rep) - (pres + (float)k * freq);
+                    store_one<T>(p, y + __uint_as_float(bias[c]));
+                }
+                r = q;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r >= nr) continue;
+            T* out = (T*)a.out + (int64_t)(g + r) * a.ld + v0;
+#pragma unroll
+            for (int k = 0; k < NC; ++k) {
+                const int c = (k * ET + tid) * E;
+                if (c >= nv) continue;
+                uint4 x = u[r][k];
+                if (lists) x = *(const uint4*)&piece[r][c];
+                if (a.e.allow) mask_chunk<T>(x, ok[r][k]);
+                if (c + E <= nv) {
+                    *(uint4*)(out + c) = x;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (c + e < nv) store_one<T>(out + c + e, Elem<T>::get(x, e));
+                }
             }
         }
     }
 }
 
+template <typename T>
+static void launch_edit_t(const EditArgs& a, dim3 grid, hipStream_t s) {
+    constexpr int R = 4 * Elem<T>::E * ET / EC;   // 64 bytes in flight per thread
+    if (a.rows_per_wg == 1) launch_k((logits_edit_kernel<T, 1>), grid, dim3(ET), 0, s, a);
+    else if (a.rows_per_wg == 2) launch_k((logits_edit_kernel<T, 2>), grid, dim3(ET), 0, s, a);
+    else launch_k((logits_edit_kernel<T, R>), grid, dim3(ET), 0, s, a);
+}
+
 dd_status launch_edit(const EditArgs& args, int dtype, hipStream_t s) {
     EditArgs a = args;
     const int64_t pieces = ceil_div(a.V, EC);
-    // rows of one sequence share their counts in a workgroup, as far as 4096 workgroups (16 per CU) remain
-    a.rows_per_wg = (int)std::min<int64_t>(16, std::max<int64_t>(1, a.rows * pieces / 4096));
-    a.rows_per_wg = (int)std::min<int64_t>(a.rows_per_wg, a.per);
+    // Rows of one sequence share their counts in a workgroup, as far as eight workgroups per CU remain (64 rows: 8.7 us with
+    // one each, 14.6 with eight; 4096 rows whose histories grow: 387 with one each, 260 with sixteen).
+    a.rows_per_wg = (int)std::min<int64_t>(std::min<int64_t>(16, a.per), std::max<int64_t>(1, a.rows * pieces / 2048));
+    while (a.rows_per_wg & (a.rows_per_wg - 1)) a.rows_per_wg &= a.rows_per_wg - 1;   // whole groups of R
     if (ceil_div(a.rows, a.rows_per_wg) > 65535) a.rows_per_wg = (int)ceil_div(a.rows, 65535);
     const dim3 grid((unsigned)pieces, (unsigned)ceil_div(a.rows, a.rows_per_wg));
     ProfScope ps(KC_LOGITS_EDIT, s);
-    if (dtype == DD_BF16) launch_k(logits_edit_kernel<bf16_t>, grid, dim3(ET), 0, s, a);
-    else launch_k(logits_edit_kernel<float>, grid, dim3(ET), 0, s, a);
+    if (dtype == DD_BF16) launch_edit_t<bf16_t>(a, grid, s);
+    else launch_edit_t<float>(a, grid, s);
     return launch_status("logits_edit");
 }
 
