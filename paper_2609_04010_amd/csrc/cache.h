@@ -53,6 +53,7 @@ struct AppendArgs {
     const void *k, *v;
     int64_t ld;
     int32_t* err;
+    bool by_row;   // set by launch_cache_append: a unit of work per row
 };
 dd_status launch_cache_append(int dtype, const AppendArgs& a, hipStream_t s);
 

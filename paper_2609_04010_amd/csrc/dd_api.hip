@@ -914,6 +914,8 @@ static dd_status cache_check(const dd_cache* c) {
 static dd_status map_check(const dd_cache_map* m) {
     DD_CHECK(m, DD_E_ARG, "map is NULL");
     DD_CHECK(m->S >= 0 && m->T >= 0 && m->ld_table >= 1, DD_E_ARG, "map sizes must not be negative, ld_table positive");
+    DD_CHECK(m->S <= (1 << 24) && m->T <= (1 << 30) && m->ld_table <= (1 << 26), DD_E_UNSUPPORTED,
+             "more than 2^24 sequences, 2^30 rows or 2^26 blocks per sequence unsupported");
     DD_CHECK(m->row_start, DD_E_ARG, "NULL pointer argument");
     DD_CHECK(m->S == 0 || (m->block_table && m->held && m->kv_len), DD_E_ARG, "NULL pointer argument");
     DD_CHECK(m->T == 0 || (m->row_seq && m->row_pos && m->slots), DD_E_ARG, "NULL pointer argument");
@@ -941,14 +943,14 @@ dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, con
     DD_CHECK(ld >= (int64_t)cache->n_kv_heads * cache->head_dim && ld * (int64_t)esize(dtype) % 16 == 0, DD_E_SHAPE,
              "ld must be >= n_kv_heads * head_dim and a multiple of 16 bytes");
     DD_CHECK(ld <= (1 << 21), DD_E_UNSUPPORTED, "ld above 2^21 unsupported");
-    DD_CHECK(((double)map->T / cache->block + 2.0 * map->S) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
+    DD_CHECK(((double)map->T / cache->block + 2.0 * map->S + 1) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
              "too many blocks: T and S are too large");
     if (map->S == 0 || map->T == 0) return DD_OK;
     DD_CHECK(codes && scales && k && v, DD_E_ARG, "NULL pointer argument");
     DD_CHECK((((uintptr_t)codes | (uintptr_t)k | (uintptr_t)v) & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
              "codes, k and v must be 16-byte aligned, scales 8-byte aligned");
     AppendArgs a = {cache_shape(cache), cache->head_dim, map->S, map->T, (uint8_t*)codes, scales, map->kv_len,
-                    map->row_start, map->row_seq, map->slots, k, v, ld, dev_err};
+                    map->row_start, map->row_seq, map->slots, k, v, ld, dev_err, false};
     return launch_cache_append(dtype, a, (hipStream_t)stream);
 }
 
@@ -1053,7 +1055,7 @@ dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, i
                          int32_t rows_per_seq, const dd_logits_edits* edits, int32_t* dev_err, void* stream) {
     DD_CHECK(logits_dtype == DD_BF16 || logits_dtype == DD_FP32, DD_E_DTYPE, "unknown logits dtype");
     DD_CHECK(rows >= 0 && V > 0 && rows_per_seq > 0, DD_E_ARG, "rows must be >= 0, V and rows_per_seq > 0");
-    DD_CHECK(V <= (1 << 24), DD_E_UNSUPPORTED, "V > 2^24 unsupported");
+    DD_CHECK(V <= (1 << 24) && rows <= (1 << 30), DD_E_UNSUPPORTED, "V > 2^24 or rows > 2^30 unsupported");
     DD_CHECK(ld >= V && ld % 8 == 0, DD_E_SHAPE, "ld must be >= V and a multiple of 8");
     DD_CHECK(edits, DD_E_ARG, "edits is NULL");
     DD_CHECK(edits->ld_history >= 0 && edits->ld_history <= INT32_MAX && edits->n_bias >= 0 && edits->n_allow >= 0, DD_E_ARG,

@@ -248,13 +248,14 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(PlanArgs a) {
 constexpr int PLAN_ROWS = 4096;
 
 dd_status launch_cache_plan(const PlanArgs& a, hipStream_t s) {
-    ProfScope ps(KC_CACHE_PLAN, s);
-    if (a.T <= PLAN_ROWS) {
-        launch_k(cache_plan_kernel<true>, dim3(1), dim3(PT), 0, s, a);
-        return launch_status("cache_plan");
+    const bool rows = a.T <= PLAN_ROWS;
+    {
+        ProfScope ps(KC_CACHE_PLAN, s);
+        if (rows) launch_k(cache_plan_kernel<true>, dim3(1), dim3(PT), 0, s, a);
+        else launch_k(cache_plan_kernel<false>, dim3(1), dim3(PT), 0, s, a);
     }
-    launch_k(cache_plan_kernel<false>, dim3(1), dim3(PT), 0, s, a);
-    ProfScope pr(KC_CACHE_PLAN, s);
+    if (rows) return launch_status("cache_plan");
+    ProfScope ps(KC_CACHE_PLAN, s);
     launch_k(cache_rows_kernel, dim3((unsigned)ceil_div(a.T, 256)), dim3(256), 0, s, a);
     return launch_status("cache_plan");
 }
@@ -265,7 +266,8 @@ dd_status launch_cache_plan(const PlanArgs& a, hipStream_t s) {
 // |x| of its rows (at most P dh numbers), fix the scale from its exponent and mantissa bits, write the codes.
 // Sequence s touches ceil((o_s + n_s) / P) blocks, o_s the place of its first new token; a wavefront finds its
 // unit by a prefix sum of those over the lanes, 64 sequences at a time, so the grid has about as many
-// units as there are (T / P + 2 S at most) and hardly a workgroup without work.
+// units as there are (T / P + 2 S at most) and hardly a workgroup without work.  (A workgroup that only finds that it
+// has nothing to do still costs about a microsecond of its CU: with one per row, 256 x 16 rows took 107 us.)
 //
 // Slabs of 32 tokens stay in registers between the maximum and the codes, so the rows are read once; W
 // wavefronts share a unit's slabs: one where sequences add few tokens (then the four wavefronts of a workgroup
@@ -515,21 +517,39 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     const int hk = W == 4 ? blockIdx.x - unit * per : (blockIdx.x - unit * per) * 4 + wave;
     if (W == 1 && hk >= 2 * a.c.H) return;
     const int values = hk >= a.c.H, h = values ? hk - a.c.H : hk;
-    int seq, j, off, r, n;
-    if (!append_find(a, unit, lane, seq, j, off, r, n)) return;
-    // rows and places of the sequence's j-th touched block
-    if (j > 0) {
-        const int skip = (j << a.c.log2p) - off;
-        r += skip;
-        n -= skip;
-        off = 0;
+    int off, r, n, slot;
+    bool bad;
+    if (a.by_row) {
+        // a unit per row: the first row of a block, or of its sequence, does the block
+        r = unit;
+        slot = a.slots[r];
+        const int seq = a.row_seq[r];
+        if (slot < 0 && seq < 0) return;   // padding
+        bad = slot < 0 || slot >= a.c.n_blocks * a.c.P || seq < 0 || seq >= a.S;
+        off = slot & (a.c.P - 1);
+        n = 0;
+        if (!bad) {
+            if (off != 0 && a.row_start[seq] != r) return;
+            n = min(a.row_start[seq + 1], a.T) - r;
+            bad = n <= 0;
+        }
+    } else {
+        int seq, j;
+        if (!append_find(a, unit, lane, seq, j, off, r, n)) return;
+        if (j > 0) {   // rows and places of the sequence's j-th touched block
+            const int skip = (j << a.c.log2p) - off;
+            r += skip;
+            n -= skip;
+            off = 0;
+        }
+        slot = a.slots[r];
+        bad = slot < 0 || slot >= a.c.n_blocks * a.c.P || (slot & (a.c.P - 1)) != off || a.row_seq[r] != seq;
     }
-    n = min(n, a.c.P - off);
-    const int slot = a.slots[r];
-    if (slot < 0 || slot >= a.c.n_blocks * a.c.P || (slot & (a.c.P - 1)) != off || a.row_seq[r] != seq) {
+    if (bad) {
         if (a.err && threadIdx.x == 0) atomicOr(a.err, DD_DEVERR_CACHE);
         return;
     }
+    n = min(n, a.c.P - off);
     const int64_t block = slot >> a.c.log2p;
     uint8_t* body = a.codes + cache_slab(a.c, DH, block, h) + (values ? (int64_t)a.c.P * DH : 0);
     float* scale = a.scales + (block * a.c.H + h) * 2 + values;
@@ -539,9 +559,12 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     else append_unit<T, DH, false, W>(x, a.ld, n, off, a.c.P, body, scale, w, red);
 }
 
-dd_status launch_cache_append(int dtype, const AppendArgs& a, hipStream_t s) {
+dd_status launch_cache_append(int dtype, const AppendArgs& args, hipStream_t s) {
+    AppendArgs a = args;
     ProfScope ps(KC_CACHE_APPEND, s);
-    const int64_t units = std::min<int64_t>(a.T, a.T / a.c.P + 2 * (int64_t)a.S);
+    // with at most two rows per sequence on average nearly every row is a unit of its own, and needs no search
+    a.by_row = a.T <= 2 * (int64_t)a.S;
+    const int64_t units = a.by_row ? a.T : std::min<int64_t>(a.T, a.T / a.c.P + 2 * (int64_t)a.S);
     // sequences that add 32 rows or more on average: four wavefronts per unit
     const bool wide = a.T >= 32 * (int64_t)a.S;
     const dim3 grid((unsigned)(units * (wide ? 2 * a.c.H : (2 * a.c.H + 3) / 4)));

@@ -67,6 +67,12 @@ def test_maps_that_are_refused(kw):
     assert _plan(_cache(), m) == 1 and _append(_cache(), m) == 1 and _attend(_cache(), m) == 1
 
 
+@pytest.mark.parametrize("kw", [dict(S=(1 << 24) + 1), dict(T=(1 << 30) + 1), dict(ld_table=(1 << 26) + 1)])
+def test_maps_that_are_too_large(kw):
+    m = _map(**kw)
+    assert _plan(_cache(), m) == 6 and _append(_cache(), m) == 6 and _attend(_cache(), m) == 6
+
+
 @pytest.mark.parametrize("name", ["seq_len", "n_new", "held", "free", "n_free", "n_free_out"])
 def test_plan_refuses_null(name):
     assert _plan(_cache(), _map(), **{name: None}) == 1
@@ -116,7 +122,7 @@ def _edit(e=None, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=5), 3), (dict(V=0), 1), (dict(rows=-1), 1), (dict(per=0), 1), (dict(ld=31), 2), (dict(ld=36), 2),
-    (dict(V=(1 << 24) + 1, ld=1 << 25), 6), (dict(logits=None), 1), (dict(out=None), 1), (dict(out=FAKE + 8), 1),
+    (dict(V=(1 << 24) + 1, ld=1 << 25), 6), (dict(rows=(1 << 30) + 1), 6), (dict(logits=None), 1), (dict(out=None), 1), (dict(out=FAKE + 8), 1),
     (dict(e="null"), 1), (dict(e=dict(ld_history=-1)), 1), (dict(e=dict(n_bias=-1)), 1), (dict(e=dict(bias_ids=FAKE)), 1),
     (dict(e=dict(bias_values=FAKE)), 1), (dict(e=dict(allow_id=FAKE)), 1), (dict(e=dict(allow=FAKE, ld_allow=1, n_allow=0)), 2),
     (dict(e=dict(allow=FAKE, ld_allow=0, n_allow=1)), 2), (dict(e=dict(n_allow=-1)), 1)])

@@ -153,7 +153,9 @@ def _pow2(torch, rng, shape, lo=-9, hi=3):
 APPEND = [  # lens, news, heads, dh, block, padding rows
     ([0], [1], 1, 32, 32, 0), ([0, 31, 32, 33], [1, 1, 1, 1], 2, 64, 32, 3), ([5, 0, 40], [70, 64, 0], 3, 64, 64, 2),
     ([100, 128, 1], [300, 128, 27], 2, 128, 128, 0), ([17, 255, 256], [250, 2, 600], 2, 128, 256, 5),
-    ([200], [1000], 2, 32, 256, 1), (list(range(40)), [3] * 40, 12, 64, 64, 0)]
+    ([200], [1000], 2, 32, 256, 1), (list(range(40)), [3] * 40, 12, 64, 64, 0),
+    (list(range(300)), [1] * 300, 1, 32, 64, 3), ([31, 0, 63] * 20, [2, 0, 3] * 20, 3, 64, 32, 0),
+    ([7] * 299 + [0], [4] * 299 + [70], 1, 64, 32, 0)]
 
 
 @pytest.mark.parametrize("lens,news,H,dh,P,pad", APPEND)
@@ -291,7 +293,10 @@ ATTEND = [  # lens, news, query heads, key heads, dh, block, padding rows
     ([1000], [1], 12, 12, 64, 64, 0), ([2000, 3, 700], [16, 16, 16], 4, 4, 64, 64, 0),
     ([5, 90, 300, 0], [7, 0, 1, 40], 8, 2, 128, 128, 3), ([70, 200], [33, 5], 6, 2, 32, 32, 2),
     ([100, 17], [130, 64], 3, 3, 64, 256, 0), ([300], [257], 16, 2, 128, 64, 0), ([4100], [3], 15, 5, 64, 32, 0),
-    ([0, 0], [40, 70], 2, 1, 32, 64, 0)]
+    ([0, 0], [40, 70], 2, 1, 32, 64, 0),
+    # enough heads for one, two and four wavefronts per column tile, and for whole sequences of more than 64 blocks
+    ([40], [70], 2100, 2100, 32, 32, 0), ([40], [70], 600, 600, 64, 32, 0), ([40], [70], 600, 600, 128, 32, 0),
+    ([400], [33], 150, 150, 32, 32, 0), ([900], [33], 150, 150, 64, 32, 2), ([2500], [1], 130, 130, 32, 32, 1)]
 
 
 @pytest.mark.parametrize("lens,news,hq,hkv,dh,P,pad", ATTEND)
@@ -321,13 +326,13 @@ def test_attention_of_strided_rows(dtype):
     assert (big[:, hq * dh:] == -7).all()
 
 
-@pytest.mark.parametrize("new", [3, 40, 100])
+@pytest.mark.parametrize("new,hkv,ctx", [(3, 2, 45), (40, 2, 45), (100, 2, 45), (35, 150, 900), (35, 150, 400), (35, 150, 45)])
 @pytest.mark.parametrize("where", ["key", "value"])
-def test_attention_nan_reaches_the_rows_that_see_it(where, new):
+def test_attention_nan_reaches_the_rows_that_see_it(where, new, hkv, ctx):
     """A NaN key (value) of a new token: rows before it are untouched, it and later rows are NaN (in that feature)."""
     torch = torch_or_skip()
     rng = np.random.default_rng(9)
-    hq, hkv, dh, P, ctx = 2, 2, 64, 32, 45
+    hq, dh, P = hkv, 64, 32
     t, codes, scales, q = _attention_case(torch, rng, [ctx], [new], hq, hkv, dh, P, "bf16", 0)
     at = ctx + new // 2
     b, o = t["table"][0, at // P], at % P
