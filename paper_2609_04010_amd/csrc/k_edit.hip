@@ -4,8 +4,9 @@
 // history's tokens and the biases of its classes, and a list of the classes that have either (whole numbers, so the
 // order of the atomics does not show).  The rows' pieces pass through LDS as they are in memory: there the listed
 // classes are edited, one per thread whatever rows they belong to, and every thread takes its 16 bytes back,
-// applies the mask to the packed numbers and stores them.  Rows of one sequence share their counts: a longer history adds its new entries, a shorter one (or another
-// sequence) begins again.
+// applies the mask to the packed numbers and stores them.  Rows of one sequence share their counts: a longer
+// history adds its new entries (those that only some of the rows edited together have are compared one by one), a
+// shorter one (or another sequence) begins again.
 //
 // Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.60 ms with any one kind of edit and
 // 0.76 ms with all (a copy 0.67 ms), 4.3 TB/s.  Of 1024, 2048 and 4096 classes and 2, 4 and 8 rows the one here was
@@ -22,6 +23,7 @@ namespace dd {
 
 constexpr int EC = 2048;   // classes of a workgroup
 constexpr int ET = 256;
+constexpr int MORE = 64;   // entries by which the histories of rows edited together may differ
 
 template <typename T> DD_DEV void store_one(T* p, float x);
 template <> DD_DEV void store_one<bf16_t>(bf16_t* p, float x) { *p = f32_to_bf16(x); }
@@ -56,6 +58,8 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
     __shared__ uint32_t some[EC / 32];                              // classes with either,
     __shared__ uint16_t list[EC];                                   // and the same as a list
     __shared__ int listed;
+    __shared__ uint16_t extra[MORE];                                // classes of the entries that only later rows of a run have
+    __shared__ int entries[R];                                      // the rows' history lengths
     const int tid = threadIdx.x;
     const int v0 = blockIdx.x * EC, nv = min(EC, a.V - v0);
     const int m0 = blockIdx.y * a.rows_per_wg, m1 = min(m0 + a.rows_per_wg, a.rows);
@@ -103,11 +107,17 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
             }
         }
         if (lists) {
-            // rows r .. q - 1 at a time that have the same history
+            if (tid < nr) entries[tid] = length(g + tid);
+            // rows r .. q - 1 at a time whose histories are the first one's with a few more entries each
             for (int r = 0; r < nr;) {
                 const int s = (g + r) / a.per, n = length(g + r);
-                int q = r + 1;
-                while (q < nr && (g + q) / a.per == s && length(g + q) == n) ++q;
+                int q = r + 1, last = n;
+                for (; q < nr && n >= 0 && (g + q) / a.per == s; ++q) {
+                    const int t = length(g + q);
+                    if (t < last || t - n > MORE) break;
+                    last = t;
+                }
+                const int more = last - n;
                 if (n >= 0 && (s != seq || n < have)) {
                     __syncthreads();         // the last rows' edits
                     for (int i = tid; i < EC / 4; i += ET) {
@@ -149,6 +159,14 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                     }
                     have = n;
                 }
+                if (more > 0) {
+                    if (r > 0) __syncthreads();   // the last rows' edits
+                    if (tid < more) {
+                        const uint32_t v = (uint32_t)a.e.history[(int64_t)s * a.e.ld_history + n + tid] - (uint32_t)v0;
+                        extra[tid] = (uint16_t)(v < (uint32_t)nv ? v : EC);
+                        if (v < (uint32_t)nv) add(v);
+                    }
+                }
                 if (r == 0) {
 #pragma unroll
                     for (int i = 0; i < R; ++i)
@@ -161,9 +179,16 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                     const int x = i / nl, c = list[i - x * nl];
                     T* p = &piece[r + x][c];
                     float y = Elem<T>::load1(p, 0);
-                    const uint32_t k = count[c];
+                    uint32_t k = count[c];
+                    if (more > 0)
+                        for (int e = 0, t = entries[r + x] - n; e < t; ++e) k += extra[e] == c;
                     if (k) y = y * (y > 0.f ? irep : rep) - (pres + (float)k * freq);
                     store_one<T>(p, y + __uint_as_float(bias[c]));
+                }
+                if (more > 0) {
+                    __syncthreads();
+                    if (tid < more && extra[tid] < EC) atomicAdd(&count[extra[tid]], 1u);
+                    have = last;
                 }
                 r = q;
             }
@@ -203,9 +228,9 @@ static void launch_edit_t(const EditArgs& a, dim3 grid, hipStream_t s) {
 dd_status launch_edit(const EditArgs& args, int dtype, hipStream_t s) {
     EditArgs a = args;
     const int64_t pieces = ceil_div(a.V, EC);
-    // Rows of one sequence share their counts in a workgroup, as far as eight workgroups per CU remain (64 rows: 8.7 us with
-    // one each, 14.6 with eight; 4096 rows whose histories grow: 387 with one each, 260 with sixteen).
-    a.rows_per_wg = (int)std::min<int64_t>(std::min<int64_t>(16, a.per), std::max<int64_t>(1, a.rows * pieces / 2048));
+    // Rows of one sequence share their counts in a workgroup, as far as three workgroups per CU remain (64 rows: 8.9 us with
+    // one each, 8.1 with two, 12.4 with eight; 4096 rows whose histories grow: 395 with one each, 221 with sixteen).
+    a.rows_per_wg = (int)std::min<int64_t>(std::min<int64_t>(16, a.per), std::max<int64_t>(1, a.rows * pieces / 800));
     while (a.rows_per_wg & (a.rows_per_wg - 1)) a.rows_per_wg &= a.rows_per_wg - 1;   // whole groups of R
     if (ceil_div(a.rows, a.rows_per_wg) > 65535) a.rows_per_wg = (int)ceil_div(a.rows, 65535);
     const dim3 grid((unsigned)pieces, (unsigned)ceil_div(a.rows, a.rows_per_wg));

@@ -49,7 +49,8 @@ def _oracle(c, keep, l):
 ALL = ("history", "hist_len", "repetition", "presence", "frequency", "bias_ids", "bias_values", "allow", "allow_id")
 EDIT = [  # sequences, rows each, V, history, biases, masks, histories that grow
     (1, 1, 1, 1, 1, 1, False), (3, 5, 37, 20, 3, 2, True), (2, 17, 4096, 300, 40, 3, True),
-    (4, 3, 4097, 1000, 7, 1, False), (2, 20, 12345, 64, 300, 4, True), (5, 1, 8190, 33, 0, 2, False)]
+    (4, 3, 4097, 1000, 7, 1, False), (2, 20, 12345, 64, 300, 4, True), (5, 1, 8190, 33, 0, 2, False),
+    (700, 16, 300, 40, 5, 3, True), (9, 64, 9000, 90, 2, 3, True)]   # several rows per workgroup
 
 
 @pytest.mark.parametrize("S,per,V,H,nb,na,grow", EDIT)
@@ -75,14 +76,38 @@ def test_edit_against_oracle(S, per, V, H, nb, na, grow, dtype, keep):
     got = got[:, :V]
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got == -np.inf, want == -np.inf)
     fin = np.isfinite(want)
-    # at most five roundings of fp32 of the largest term on the way, then one to the type
+    # at most six roundings of fp32 on the way (1 / repetition, its product, count * frequency, + presence, the difference,
+    # + bias), each half a step of no more than the largest term, then one to the type
     term = np.abs(np.where(np.isfinite(l), l, 0)) * 1.6 + 0.5 + 0.3 * H + 16
-    tol = np.abs(np.where(fin, want, 0)) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) + 5 * 2.0 ** -24 * term
+    tol = np.abs(np.where(fin, want, 0)) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) + 6 * 2.0 ** -24 * term
     d = np.abs(np.where(fin, got, 0) - np.where(fin, want, 0))
     assert (d <= tol).all(), float((d / tol).max())
     dd.logits_edit(x, dtype, ld, rows, V, x, per, **a)                    # in place
     assert torch.equal(torch.nan_to_num(x[:, :V].float()), torch.nan_to_num(out[:, :V].float()))
     assert ld == V or (x[:, V:] == 5).all()
+
+
+@pytest.mark.parametrize("steps", [[3, 3, 3, 3], [0, 70, 0, 5], [5, -2, 9, 1], [64, 64, 65, 1]])
+def test_edit_of_histories_that_jump(steps):
+    """Rows edited together whose histories grow by much, shrink, or stand still, between rows that pass."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(17)
+    S, per, V, H = 600, 16, 300, 1100
+    c = _case(rng, S, per, V, H, 3, 1, False)
+    c["history"] = rng.integers(0, 40, (S, H))
+    n = np.cumsum(np.resize(steps, per)) + 5
+    c["hist_len"] = np.tile(n, S)
+    c["hist_len"][::7] = -1
+    l = round_to_dtype(rng.normal(size=(S * per, V)) * 3, "fp32")
+    x, out = logits_dev(torch, l, "fp32", 304), dev_i32(torch, [0])
+    out, err = torch.zeros_like(x), out
+    keep = ("history", "hist_len", "repetition", "presence", "frequency", "bias_ids", "bias_values")
+    dd.logits_edit(x, "fp32", 304, S * per, V, out, per, dev_err=err, **_args(torch, c, keep))
+    want = _oracle(c, keep, l)
+    got = out[:, :V].double().cpu().numpy()
+    assert int(err.item()) == 0
+    term = np.abs(l) * 1.6 + 0.5 + 0.3 * H + 16               # as in test_edit_against_oracle
+    assert (np.abs(got - want) <= np.abs(want) * 2.0 ** -24 + 6 * 2.0 ** -24 * term).all()
 
 
 def test_edit_of_rows_past_the_last_whole_sequence_and_bad_mask_numbers():
