@@ -19,6 +19,7 @@ Modules, each written from the paper (arXiv 2609.04010) and cited per function:
   sampler    two-level Gumbel-max categorical sampling
   latent     Gaussian-latent argmax and the alpha_tilde <-> alpha map
   loop       the T-step ancestral sampling loop
+  cache      the cached context of a serving pass, edits of logits
 
 Parity status of each function is listed in its module header; the forward
 pass has no paper-fixed values and is pinned by invariants and by a second
