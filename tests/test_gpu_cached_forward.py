@@ -233,3 +233,21 @@ def test_cached_forward_in_a_graph():
         assert torch.equal(a.logits[:k], b.logits[:k]) and torch.equal(a.m.kv_len, b.m.kv_len)
         assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
     assert dd.read_device_error(b.ws[:4].view(torch.int32)) == 0
+
+
+def test_profiler_counts_the_launches():
+    torch = torch_or_skip()
+    cfg = workloads.model_cfg(2, n_layers=2, vocab=300, max_len=256)
+    sv = Server(torch, cfg, 15, S=1, T=20, n_blocks=4, P=32, ld_table=3)
+    z = dev_i32(torch, np.arange(20))
+    dd.profile_begin(200, ["cache_plan", "cache_append", "cache_attention", "logits_edit"])
+    try:
+        dd.cache_plan(sv.cc, sv.m, sv.length, dev_i32(torch, [20]), sv.m.held, sv.free, sv.n_free, sv.n_free)
+        dd.denoise_forward_cached(cfg, sv.params, z, 1.0, sv.cc, sv.codes, sv.scales, sv.m, sv.logits, sv.ldl, sv.ws, 20, sv.max_kv)
+        dd.logits_edit(sv.logits, "bf16", sv.ldl, 20, 300, sv.logits)
+    finally:
+        dd.profile_end()
+    got = dd.profile_read()
+    say(got)
+    assert {k: v[0] for k, v in got.items()} == {"cache_plan": 1, "cache_append": 2, "cache_attention": 2, "logits_edit": 1}
+    assert all(v[1] > 0 for v in got.values())
