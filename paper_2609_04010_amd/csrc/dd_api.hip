@@ -935,6 +935,13 @@ dd_status dd_cache_plan(const dd_cache* cache, const dd_cache_map* map, const in
     return launch_cache_plan(a, (hipStream_t)stream);
 }
 
+// Whether a pass's touched blocks and heads fit a grid.
+static dd_status append_size_check(const dd_cache* cache, int32_t S, int32_t T) {
+    DD_CHECK(((double)T / cache->block + 2.0 * S + 1) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
+             "too many blocks: T and S are too large");
+    return DD_OK;
+}
+
 dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, const dd_cache_map* map, const void* k,
                           const void* v, int32_t dtype, int64_t ld, int32_t* dev_err, void* stream) {
     DD_TRY(cache_check(cache));
@@ -943,8 +950,7 @@ dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, con
     DD_CHECK(ld >= (int64_t)cache->n_kv_heads * cache->head_dim && ld * (int64_t)esize(dtype) % 16 == 0, DD_E_SHAPE,
              "ld must be >= n_kv_heads * head_dim and a multiple of 16 bytes");
     DD_CHECK(ld <= (1 << 21), DD_E_UNSUPPORTED, "ld above 2^21 unsupported");
-    DD_CHECK(((double)map->T / cache->block + 2.0 * map->S + 1) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
-             "too many blocks: T and S are too large");
+    DD_TRY(append_size_check(cache, map->S, map->T));
     if (map->S == 0 || map->T == 0) return DD_OK;
     DD_CHECK(codes && scales && k && v, DD_E_ARG, "NULL pointer argument");
     DD_CHECK((((uintptr_t)codes | (uintptr_t)k | (uintptr_t)v) & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
@@ -1013,6 +1019,8 @@ static dd_status cached_check(const dd_config* cfg, const dd_cache* cache, int32
     DD_TRY(cfg_check(cfg));
     DD_TRY(forward_check(cfg));
     DD_TRY(cache_attn_check(cache, S, T, cfg->n_heads, max_new, max_kv));
+    DD_TRY(append_size_check(cache, S, T));
+    DD_CHECK(cfg->d_model <= (1 << 19), DD_E_UNSUPPORTED, "d_model above 2^19 unsupported");
     DD_CHECK(cache->n_kv_heads == cfg->n_heads && cache->head_dim == cfg->d_model / cfg->n_heads, DD_E_SHAPE,
              "the cache holds %d heads of %d, the model has %d of %d", cache->n_kv_heads, cache->head_dim,
              cfg->n_heads, cfg->d_model / cfg->n_heads);

@@ -429,10 +429,11 @@ static constexpr AttnShape SHAPES[] = {{8, 1}, {4, 1}, {2, 2}, {1, 4}};
 // Wavefronts per column tile: as many as leave some six wavefronts per SIMD in all (three of the larger ones of
 // head dimension 128), since a tile's chain of loads, products and exponentials wants others beside it; but where the
 // column tiles alone give every CU work, at least six tiles of tokens each (the first loads and the meeting in
-// LDS cost about as much as two).  Measured, us, with 8 | 4 | 2 | 1: 3072 column tiles of causal prompts over 4096
-// tokens - | 109 | 100 | 105; 2048 tiles of head dimension 128 over 1500 tokens - | 72 | 65 | 61; 768 tiles (64 x 16
-// rows, 12 heads, 4096 tokens) 56 | 56 | 59 | -; 768 tiles over 1024 tokens 21 | 18 | 19 | -; 320 tiles (2 x 300 rows,
-// 16 heads, 900 tokens) 13 | 10 | 12 | 20; 192 tiles (8 x 40 rows, 12 heads, 4096 tokens) 18 | 20 | 22 | 33.
+// LDS cost about as much as two).  Measured, us, with 8 | 4 | 2 | 1: causal prompts of 4 x 2048 rows, 12 heads, over
+// 4096 tokens - | 109 | 100 | 105; 2048 column tiles of head dimension 128 over 1500 tokens - | 72 | 65 | 61; 768 tiles
+// (64 x 16 rows, 12 heads, 4096 tokens) 56 | 56 | 59 | -; 768 tiles over 1024 tokens 21 | 18 | 19 | -; 320 tiles
+// (2 x 300 rows, 16 heads, 900 tokens) 13 | 10 | 12 | 20; 192 tiles (8 x 40 rows, 12 heads, 4096 tokens)
+// 18 | 20 | 22 | 33.
 // Pieces: cutting a sequence costs the partial results' way through memory and a second launch (768 tiles:
 // 56 us whole, 73 in two), so it is done only while the workgroups are fewer than half the CUs, for pieces of 1024
 // tokens and more (1 row, 8 heads, 32768 tokens: 20 us in 16 pieces, 27 in 8; 12 heads, 1001 tokens: 7.1 us whole,
@@ -441,7 +442,7 @@ CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int
     CacheAttnPlan p;
     const int64_t cols = (int64_t)max_new * (Hq / Hkv), per = std::max<int64_t>(1, (int64_t)S * Hkv);
     const int64_t tiles = std::max<int64_t>(1, per * ceil_div(cols, 32));
-    int64_t waves = (dh > 64 ? 3072 : 6144) / tiles;
+    int64_t waves = (dh > 64 ? 3200 : 6400) / tiles;
     if (tiles > 256) waves = std::min(waves, ceil_div(max_kv, 32) / 6);
     p.shape = waves >= 8 ? 0 : waves >= 4 ? 1 : waves >= 2 ? 2 : 3;
     const AttnShape sh = SHAPES[p.shape];

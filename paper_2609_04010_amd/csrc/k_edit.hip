@@ -12,8 +12,6 @@
 // 0.76 ms with all (a copy 0.67 ms), 4.3 TB/s.  Of 1024, 2048 and 4096 classes and 2, 4 and 8 rows the one here was
 // fastest (0.81 to 1.03 ms).  Every global load of the R rows is on its way before one is waited for: a wait for a
 // row's mask number between them cost 0.3 ms.
-#include <math.h>
-
 #include <algorithm>
 
 #include "cache.h"
