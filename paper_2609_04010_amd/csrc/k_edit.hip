@@ -8,10 +8,10 @@
 // history adds its new entries (those that only some of the rows edited together have are compared one by one), a
 // shorter one (or another sequence) begins again.
 //
-// Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.60 ms with any one kind of edit and
-// 0.76 ms with all (a copy 0.67 ms), 4.3 TB/s.  Of 1024, 2048 and 4096 classes and 2, 4 and 8 rows the one here was
-// fastest (0.81 to 1.03 ms).  Every global load of the R rows is on its way before one is waited for: a wait for a
-// row's mask number between them cost 0.3 ms.
+// Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.62 ms with every kind of edit (0.59 to
+// 0.61 with any one kind, a copy 0.67 ms), 5.3 TB/s.  2048 classes and 4 rows at a time (8 rows: the same time, twice
+// the LDS; 4096 classes: 3 % slower).  No row waits for its own history length or mask number: the lanes read those
+// of 64 rows at once (read row by row, 0.77 ms).
 #include <algorithm>
 
 #include "cache.h"
@@ -65,16 +65,23 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
     const bool lists = a.e.ld_history > 0 || biased;   // some class may need its logit changed
     int seq = -1, have = 0;   // sequence whose tables stand in LDS, entries counted
     float rep = 1.f, irep = 1.f, pres = 0.f, freq = 0.f;
-    auto length = [&](int m) {   // history entries of a row; negative: the row goes through as it is
+    // history lengths (negative: the row goes through as it is) and mask numbers of 64 rows, one per lane: no row
+    // waits for its own
+    int lens = 0, masks = 0;
+    auto window = [&](int g) {
+        const int m = min(g + (tid & 63), m1 - 1);
         const int64_t n = a.e.hist_len ? a.e.hist_len[m] : a.e.ld_history;
-        return (int)(n < a.e.ld_history ? n : a.e.ld_history);
+        lens = (int)(n < a.e.ld_history ? n : a.e.ld_history);
+        masks = a.e.allow_id ? a.e.allow_id[m] : 0;
     };
+    auto length = [&](int m) { return __builtin_amdgcn_readlane(lens, (m - m0) & 63); };
     auto add = [&](uint32_t v) {   // class v of this piece into the list
         const uint32_t bit = 1u << (v & 31u);
         if (!(atomicOr(&some[v >> 5], bit) & bit)) list[atomicAdd(&listed, 1)] = (uint16_t)v;
     };
     for (int g = m0; g < m1; g += R) {
         const int nr = min(R, m1 - g);
+        if (((g - m0) & 63) == 0) window(g);
         uint4 u[R][NC];
         uint32_t ok[R][NC];
 #pragma unroll
@@ -85,18 +92,12 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                 u[r][k] = *(const uint4*)(in + min((k * ET + tid) * E, (nv - 1) & ~(E - 1)));
         }
         if (a.e.allow) {
-            int id[R], len[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {   // all of them on the way before one is looked at
-                const int m = min(g + r, m1 - 1);
-                id[r] = a.e.allow_id ? a.e.allow_id[m] : 0;
-                len[r] = a.e.hist_len ? a.e.hist_len[m] : 0;
-            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const bool in = id[r] >= 0 && id[r] < a.e.n_allow, every = !in || len[r] < 0;
-                if (!in && id[r] != -1 && len[r] >= 0 && a.err && tid == 0 && blockIdx.x == 0) atomicOr(a.err, DD_DEVERR_MASK);
-                const uint32_t* allow = a.e.allow + (in ? (int64_t)id[r] * a.e.ld_allow : 0);
+                const int m = min(g + r, m1 - 1), id = __builtin_amdgcn_readlane(masks, (m - m0) & 63), len = length(m);
+                const bool in = id >= 0 && id < a.e.n_allow, every = !in || len < 0;
+                if (!in && id != -1 && len >= 0 && a.err && tid == 0 && blockIdx.x == 0) atomicOr(a.err, DD_DEVERR_MASK);
+                const uint32_t* allow = a.e.allow + (in ? (int64_t)id * a.e.ld_allow : 0);
 #pragma unroll
                 for (int k = 0; k < NC; ++k) {
                     const int v = v0 + min((k * ET + tid) * E, (nv - 1) & ~(E - 1));
@@ -105,7 +106,8 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
             }
         }
         if (lists) {
-            if (tid < nr) entries[tid] = length(g + tid);
+            const int mine = __shfl(lens, (g - m0 + tid) & 63, 64);
+            if (tid < nr) entries[tid] = mine;
             // rows r .. q - 1 at a time whose histories are the first one's with a few more entries each
             for (int r = 0; r < nr;) {
                 const int s = (g + r) / a.per, n = length(g + r);
@@ -226,8 +228,8 @@ static void launch_edit_t(const EditArgs& a, dim3 grid, hipStream_t s) {
 dd_status launch_edit(const EditArgs& args, int dtype, hipStream_t s) {
     EditArgs a = args;
     const int64_t pieces = ceil_div(a.V, EC);
-    // Rows of one sequence share their counts in a workgroup, as far as three workgroups per CU remain (64 rows: 8.9 us with
-    // one each, 8.1 with two, 12.4 with eight; 4096 rows whose histories grow: 395 with one each, 221 with sixteen).
+    // Rows of one sequence share their counts in a workgroup, as far as three workgroups per CU remain (64 rows: 8.7 us with
+    // one each, 7.9 with two, 11.1 with eight; 4096 rows whose histories grow: 404 with one each, 183 with sixteen).
     a.rows_per_wg = (int)std::min<int64_t>(std::min<int64_t>(16, a.per), std::max<int64_t>(1, a.rows * pieces / 800));
     while (a.rows_per_wg & (a.rows_per_wg - 1)) a.rows_per_wg &= a.rows_per_wg - 1;   // whole groups of R
     if (ceil_div(a.rows, a.rows_per_wg) > 65535) a.rows_per_wg = (int)ceil_div(a.rows, 65535);
