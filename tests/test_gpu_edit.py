@@ -110,6 +110,33 @@ def test_edit_of_histories_that_jump(steps):
     assert (np.abs(got - want) <= np.abs(want) * 2.0 ** -24 + 6 * 2.0 ** -24 * term).all()
 
 
+def test_edit_of_more_rows_than_the_grid_is_high():
+    """More than 64 rows in each workgroup; whole numbers and halves, so nothing is rounded."""
+    torch = torch_or_skip()
+    rows, V, per, H, na = 65535 * 66 + 5, 5, 1000, 4, 7
+    ld, S = int(dd.logits_ld(V)), -(-rows // per)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    draw = lambda lo, hi, *shape: torch.randint(lo, hi, shape, generator=g, device="cuda", dtype=torch.int32)   # noqa: E731
+    x = draw(-8, 9, rows, ld).to(torch.bfloat16)
+    history, hist_len = draw(0, V, S, H), draw(-1, H + 1, rows)
+    allow, allow_id = draw(0, 2 ** V, na, 1), draw(-1, na, rows)
+    presence = torch.full((S,), 0.5, device="cuda")
+    say("edit rows", rows)
+    out = torch.empty_like(x)
+    dd.logits_edit(x, "bf16", ld, rows, V, out, per, history=history, hist_len=hist_len, presence=presence, allow=allow,
+                   allow_id=allow_id)
+    seq = torch.arange(rows, device="cuda") // per
+    bits = (allow >> torch.arange(V, device="cuda", dtype=torch.int32)) & 1
+    want = x[:, :V].float()
+    named = torch.zeros_like(want, dtype=torch.bool)
+    for i in range(H):
+        named |= (history[seq, i, None] == torch.arange(V, device="cuda")) & (hist_len > i)[:, None]
+    want = want - 0.5 * named
+    shut = (bits[allow_id.clamp(min=0).long()] == 0) & (allow_id >= 0)[:, None] & (hist_len >= 0)[:, None]
+    want = torch.where(shut, torch.full_like(want, -np.inf), want)
+    assert torch.equal(out[:, :V].float(), want)
+
+
 def test_edit_of_rows_past_the_last_whole_sequence_and_bad_mask_numbers():
     torch = torch_or_skip()
     rng = np.random.default_rng(3)
