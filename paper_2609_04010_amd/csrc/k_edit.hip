@@ -160,7 +160,7 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                     have = n;
                 }
                 if (more > 0) {
-                    if (r > 0) __syncthreads();   // the last rows' edits
+                    if (r > 0 || n == 0) __syncthreads();   // the last rows' edits; the biases, where no entry was counted
                     if (tid < more) {
                         const uint32_t v = (uint32_t)a.e.history[(int64_t)s * a.e.ld_history + n + tid] - (uint32_t)v0;
                         extra[tid] = (uint16_t)(v < (uint32_t)nv ? v : EC);
