@@ -64,7 +64,7 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
     const bool biased = a.e.bias_ids != nullptr && a.e.n_bias > 0;
     const bool lists = a.e.ld_history > 0 || biased;   // some class may need its logit changed
     int seq = -1, have = 0;   // sequence whose tables stand in LDS, entries counted
-    float rep = 1.f, irep = 1.f, pres = 0.f, freq = 0.f;
+    float rep = 1.f, pres = 0.f, freq = 0.f;
     // history lengths (negative: the row goes through as it is) and mask numbers of 64 rows, one per lane: no row
     // waits for its own
     int lens = 0, masks = 0;
@@ -142,7 +142,6 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                         }
                     }
                     rep = a.e.repetition ? a.e.repetition[s] : 1.f;
-                    irep = 1.f / rep;
                     pres = a.e.presence ? a.e.presence[s] : 0.f;
                     freq = a.e.frequency ? a.e.frequency[s] : 0.f;
                     seq = s;
@@ -182,7 +181,7 @@ __global__ __launch_bounds__(ET) void logits_edit_kernel(EditArgs a) {
                     uint32_t k = count[c];
                     if (more > 0)
                         for (int e = 0, t = entries[r + x] - n; e < t; ++e) k += extra[e] == c;
-                    if (k) y = y * (y > 0.f ? irep : rep) - (pres + (float)k * freq);
+                    if (k) y = (y > 0.f ? y / rep : y * rep) - (pres + (float)k * freq);
                     store_one<T>(p, y + __uint_as_float(bias[c]));
                 }
                 if (more > 0) {
