@@ -97,6 +97,12 @@ DD_DEV float max_halves(float v) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Values enter the products times 2^-16 and the result leaves times 2^16.  Scales go up to 2^120: as they stand, codes of
+// 256 and more would be infinite in bf16 (and, in places behind the last token, 0 * inf), and sums of 2^8 times a value, or
+// of many values, pass fp32's end before the division.  With it every code is finite, a sum of weights
+// may reach 2^16 at the largest value (2^32 at 2^112), and the smallest code, 2^-109, is 2^-125, still a normal number.
+constexpr float V_DOWN = 0x1p-16f, V_UP = 0x1p16f;
+
 // KW wavefronts share a column tile, CW column tiles side by side, NB tiles of tokens in a wavefront's registers
 // (NB - 1 ahead of the one in work).
 template <typename T, int DH, int KW, int CW, int NB>
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(64 * KW * CW) void cache_attn_kernel(CacheAttnArgs 
         const int b = (tile0 >> a.c.log2p) - bw;
         if (__builtin_amdgcn_readlane(id, b) < 0) return;
         const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), b));
-        const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), b));
+        const float vs = V_DOWN * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), b));
         f32x16 sT = {};
 #pragma unroll
         for (int st = 0; st < KS; ++st) {
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(64 * KW * CW) void cache_attn_kernel(CacheAttnArgs 
     // four consecutive features of a column, normalised into out or, of a cut sequence, as they are
     auto put = [&](int rw, int hd, int d, float4 v, float sum) {
         if (whole) {
-            store4<T>((T*)a.out + (int64_t)rw * a.ldo + (int64_t)hd * DH + d, scaled(v, sum == 0.f ? 0.f : 1.f / sum));
+            store4<T>((T*)a.out + (int64_t)rw * a.ldo + (int64_t)hd * DH + d, scaled(v, sum == 0.f ? 0.f : V_UP / sum));
         } else {
             *(float4*)(a.part + (((int64_t)rw * a.Hq + hd) * a.nsplit + piece) * DH + d) = v;
         }
@@ -417,7 +423,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(CacheAttnArgs a) {
         v.w += __shfl_xor(v.w, d, 64);
     }
     if (pg == 0)
-        store4<T>((T*)a.out + (int64_t)(r0 + i) * a.ldo + (int64_t)head * DH + f4 * 4, scaled(v, sum == 0.f ? 0.f : 1.f / sum));
+        store4<T>((T*)a.out + (int64_t)(r0 + i) * a.ldo + (int64_t)head * DH + f4 * 4, scaled(v, sum == 0.f ? 0.f : V_UP / sum));
 }
 
 // Shapes of a workgroup: wavefronts that share a column tile, column tiles side by side.
