@@ -544,7 +544,7 @@ typedef struct {
  * The call does all of this or, where something does not fit, nothing: then DD_DEVERR_CACHE is set, no
  * block changes hands, held, kv_len and n_free_out take held, seq_len and *n_free, and every row is
  * padding.  That is so where the pool has too few blocks, the new tokens are more than T, a sequence
- * would pass ld_table * P tokens, or an input is no plan's (a negative length, n_new below -1, seq_len
+ * would pass ld_table * P or 2^31 - 1 tokens, or an input is no plan's (a negative length, n_new below -1, seq_len
  * beyond held * P, *n_free outside [0, n_blocks], more blocks given back than the stack has room for).
  * A block number outside [0, n_blocks) in a table row that gets new tokens or in the stack sets
  * DD_DEVERR_CACHE; the rows concerned get slot -1.

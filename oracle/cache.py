@@ -56,7 +56,7 @@ def plan(n_blocks, P, ld_table, T, seq_len, n_new, held, table, free, n_free):
             need.append(0)
         else:
             total = seq_len[s] + n_new[s]
-            fit = fit and total <= ld_table * P
+            fit = fit and total <= min(ld_table * P, 2 ** 31 - 1)
             need.append(max(0, -(-total // P) - held[s]))
     rows = sum(max(0, int(n)) for n in n_new)
     fit = fit and rows <= T and n_free + give <= n_blocks and sum(need) <= n_free + give

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(PT) void cache_plan_kernel(PlanArgs a) {
             x[2] = held;
             return true;
         }
-        if (total > (int64_t)a.ld_table * a.c.P) return false;
+        if (total > min((int64_t)a.ld_table * a.c.P, (int64_t)INT32_MAX)) return false;   // (a table may reach past 32-bit positions)
         x[0] = n;
         x[1] = max(0, (int32_t)((total + P1) >> lp) - held);
         return true;
