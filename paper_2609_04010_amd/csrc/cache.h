@@ -53,8 +53,14 @@ struct AppendArgs {
     const void *k, *v;
     int64_t ld;
     int32_t* err;
-    bool by_row;   // set by launch_cache_append: a unit of work per row
+    bool by_row;   // set by launch_cache_append, from its grid
 };
+// How a call is cut: a unit of work per row or per touched block, and whether its keys or values have a workgroup of their own.
+struct AppendGrid {
+    bool by_row, wide;
+    int64_t wgs;
+};
+AppendGrid cache_append_grid(int32_t S, int32_t T, int32_t P, int32_t H);
 dd_status launch_cache_append(int dtype, const AppendArgs& a, hipStream_t s);
 
 struct CacheAttnArgs {
@@ -79,6 +85,7 @@ struct CacheAttnArgs {
 // tokens per workgroup and how many such pieces max_kv has, bytes of partial results.
 struct CacheAttnPlan {
     int shape, chunk, nsplit;
+    int threads;   // of a workgroup
     int64_t tiles;
     size_t ws;
 };

@@ -128,6 +128,9 @@ inline void launch_k(void (*k)(KP...), dim3 grid, dim3 block, uint32_t shmem, hi
         args);
 }
 
+// Whether a launch of this many workgroups is one that the runtime takes: below 2^32 work-items.
+inline bool grid_fits(double workgroups, int threads) { return workgroups * threads < 4294967296.0; }
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace dd

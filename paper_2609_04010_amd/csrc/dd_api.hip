@@ -937,7 +937,7 @@ dd_status dd_cache_plan(const dd_cache* cache, const dd_cache_map* map, const in
 
 // Whether a pass's touched blocks and heads fit a grid.
 static dd_status append_size_check(const dd_cache* cache, int32_t S, int32_t T) {
-    DD_CHECK(((double)T / cache->block + 2.0 * S + 1) * 2 * cache->n_kv_heads < 2147483647.0, DD_E_UNSUPPORTED,
+    DD_CHECK(grid_fits((double)cache_append_grid(S, T, cache->block, cache->n_kv_heads).wgs, 256), DD_E_UNSUPPORTED,
              "too many blocks: T and S are too large");
     return DD_OK;
 }
@@ -972,8 +972,8 @@ static dd_status cache_attn_check(const dd_cache* cache, int32_t S, int32_t T, i
     if (S == 0 || T == 0) return DD_OK;
     const CacheAttnPlan p = cache_attn_plan(S, T, cache->n_kv_heads, n_heads, cache->head_dim, max_new, max_kv);
     const double wgs = ((double)S * cache->n_kv_heads * p.nsplit + 8) * (double)p.tiles;
-    DD_CHECK(wgs < 2147483647.0 && (double)S * max_new * n_heads < 2147483647.0, DD_E_UNSUPPORTED,
-             "too many workgroups: S * max_new * n_heads is too large");
+    // (the launch that joins pieces is small: sequences are cut only where the workgroups are few)
+    DD_CHECK(grid_fits(wgs, p.threads), DD_E_UNSUPPORTED, "too many workgroups: S * max_new * n_heads is too large");
     return DD_OK;
 }
 
@@ -1025,6 +1025,7 @@ static dd_status cached_check(const dd_config* cfg, const dd_cache* cache, int32
              "the cache holds %d heads of %d, the model has %d of %d", cache->n_kv_heads, cache->head_dim,
              cfg->n_heads, cfg->d_model / cfg->n_heads);
     DD_CHECK(max_kv <= cfg->max_len, DD_E_SHAPE, "max_kv = %d exceeds max_len = %d", max_kv, cfg->max_len);
+    DD_CHECK(grid_fits(ceil_div(T, 4), 256), DD_E_UNSUPPORTED, "T = %d: rows of the denoiser are limited to 2^26", T);
     return DD_OK;
 }
 

@@ -559,18 +559,26 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a) {
     else append_unit<T, DH, false, W>(x, a.ld, n, off, a.c.P, body, scale, w, red);
 }
 
+AppendGrid cache_append_grid(int32_t S, int32_t T, int32_t P, int32_t H) {
+    AppendGrid g;
+    // with at most two rows per sequence on average nearly every row is a unit of its own, and needs no search
+    g.by_row = T <= 2 * (int64_t)S;
+    const int64_t units = g.by_row ? T : std::min<int64_t>(T, T / P + 2 * (int64_t)S);
+    // sequences that add 32 rows or more on average: four wavefronts per unit
+    g.wide = T >= 32 * (int64_t)S;
+    g.wgs = units * (g.wide ? 2 * H : (2 * H + 3) / 4);
+    return g;
+}
+
 dd_status launch_cache_append(int dtype, const AppendArgs& args, hipStream_t s) {
     AppendArgs a = args;
     ProfScope ps(KC_CACHE_APPEND, s);
-    // with at most two rows per sequence on average nearly every row is a unit of its own, and needs no search
-    a.by_row = a.T <= 2 * (int64_t)a.S;
-    const int64_t units = a.by_row ? a.T : std::min<int64_t>(a.T, a.T / a.c.P + 2 * (int64_t)a.S);
-    // sequences that add 32 rows or more on average: four wavefronts per unit
-    const bool wide = a.T >= 32 * (int64_t)a.S;
-    const dim3 grid((unsigned)(units * (wide ? 2 * a.c.H : (2 * a.c.H + 3) / 4)));
+    const AppendGrid g = cache_append_grid(a.S, a.T, a.c.P, a.c.H);
+    a.by_row = g.by_row;
+    const dim3 grid((unsigned)g.wgs);
 #define X(T, d)                                                                          \
     if (a.dh == d) {                                                                     \
-        if (wide) launch_k((cache_append_kernel<T, d, 4>), grid, dim3(256), 0, s, a);    \
+        if (g.wide) launch_k((cache_append_kernel<T, d, 4>), grid, dim3(256), 0, s, a);    \
         else launch_k((cache_append_kernel<T, d, 1>), grid, dim3(256), 0, s, a);         \
         return launch_status("cache_append");                                            \
     }

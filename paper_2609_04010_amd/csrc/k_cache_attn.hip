@@ -452,6 +452,7 @@ CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int
     if (tiles > 256) waves = std::min(waves, ceil_div(max_kv, 32) / 6);
     p.shape = waves >= 8 ? 0 : waves >= 4 ? 1 : waves >= 2 ? 2 : 3;
     const AttnShape sh = SHAPES[p.shape];
+    p.threads = 64 * sh.kw * sh.cw;
     p.tiles = ceil_div(cols, 32 * sh.cw);
     const int64_t wgs = per * p.tiles;
     int64_t chunk = ceil_div(max_kv, 32) * 32;
