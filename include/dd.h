@@ -609,7 +609,7 @@ dd_status dd_cache_attention(const dd_cache* cache, const void* codes, const flo
  * its part of the cache and attends over it.
  *   z_t          device int32 [T], the token of each row; padding rows' tokens are not looked at
  *   alpha_t      conditions the time embedding (1 for a clean context and its verification)
- *   cache        n_kv_heads = cfg->n_heads, head_dim = d_model / n_heads
+ *   cache        n_kv_heads = cfg->n_heads, head_dim = d_model / n_heads (one that dd_denoise_forward takes)
  *   codes, scales  the cache of every layer in turn: [n_layers] of what dd_cache describes
  *   map          of dd_cache_plan, run before this call on the same stream; positions beyond max_len set
  *                DD_DEVERR_CACHE

@@ -27,7 +27,7 @@ DD_DEV int wave_sum_int(int v) {
 // anything is written), once for the blocks given back (only if there are any), once for rows and
 // blocks taken.  Inside such a piece the items (blocks, rows) are spread over the threads, which find
 // their sequence by bisection of the prefix sums in LDS.  Bound by latency: a chain of two or three loads, a few
-// scans and the stores, 6.1 us for 16 sequences of one token, 12.4 us (with the rows' own launch) for 1024
+// scans and the stores, 6.0 us for 16 sequences of one token, 14.1 us (with the rows' own launch) for 1024
 // sequences of 16 drafted tokens, some prompts and some ends, 65536 rows.
 constexpr int PT = 1024;           // threads, and sequences of a piece
 

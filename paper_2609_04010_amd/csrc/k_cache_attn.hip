@@ -17,16 +17,19 @@
 // 32 i + 16 g .. + 15, steps 2 i and 2 i + 1.
 //
 // fp32 rows: q (and the probabilities) are taken as the sum of three bf16 numbers of 8 bits each, which is
-// exact, one product each.
+// exact, one product each.  bf16 rows: the probabilities are rounded to bf16 for the product with V (their sum is not):
+// another bf16 number of theirs would cost another product, and the result is rounded to bf16 in any case.  0.0020 off
+// the 64-bit result (in norm), where fp32 probabilities give 0.0017.
 //
 // KW wavefronts of a workgroup share a column tile and take every KW-th tile of tokens; their results meet in
 // LDS.  Where that leaves CUs idle, long caches are cut into pieces of `chunk` tokens over workgroups whose
 // partial results cache_attn_join_kernel adds.
 //
 // Bound: few columns per key head, by the bytes of the cache (32 rows, 8 heads of 128, 16384 to 32768 tokens:
-// 1.61 GB in 302 us, 5.3 TB/s, where reading such blocks and nothing else reaches 6.0; 64 x 16 rows, 12 heads of 64,
-// 2048 to 4112 tokens: 303 MB in 56 us, 5.4 TB/s); many columns, by the vector instructions between the products
-// (about 590 cycles per 32 x 32 tile, 256 of matrix instructions: prompts of 4 x 2048 rows, 64 GFLOP in 102 us).
+// 1.61 GB in 301 us, 5.4 TB/s, where reading such blocks and nothing else reaches 6.0; 64 x 16 rows, 12 heads of 64,
+// 2048 to 4112 tokens: 307 MB in 60 us, 5.1 TB/s); many columns, by the vector instructions between the products
+// (about 590 cycles per 32 x 32 tile, 256 of matrix instructions: prompts of 4 x 2048 rows, 64 GFLOP in 97 us).  Times
+// here and below are those of calls that follow each other.
 #include <math.h>
 
 #include <algorithm>

@@ -8,8 +8,8 @@
 // history adds its new entries (those that only some of the rows edited together have are compared one by one), a
 // shorter one (or another sequence) begins again.
 //
-// Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.62 ms with every kind of edit (0.59 to
-// 0.61 with any one kind, a copy 0.67 ms), 5.3 TB/s.  2048 classes and 4 rows at a time (8 rows: the same time, twice
+// Bound by the memory traffic of the logits: 16384 rows of 50257 bf16 take 0.61 ms with every kind of edit (0.59 to
+// 0.61 with any one kind, a copy 0.67 ms), 5.4 TB/s.  2048 classes and 4 rows at a time (8 rows: the same time, twice
 // the LDS; 4096 classes: 3 % slower).  No row waits for its own history length or mask number: the lanes read those
 // of 64 rows at once (read row by row, 0.77 ms).
 #include <algorithm>
