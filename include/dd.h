@@ -592,7 +592,8 @@ dd_status dd_cache_append(const dd_cache* cache, void* codes, float* scales, con
  * key or value reaches the rows that see its token and no others.
  * Arithmetic: products of exact e4m3 values with q in bf16 (fp32 q as the sum of three bf16 numbers),
  * fp32 sums and softmax; the probabilities enter the product with v as q does (rounded to bf16, or the
- * sum of three).  Values are summed times 2^-16, so that none that the cache can hold overflows on the way.
+ * sum of three).  Values are summed times 2^-16: weights, each up to 2^8, may add to
+ * 2^16 at the largest value before a sum passes fp32's end.
  */
 size_t dd_cache_attention_workspace_bytes(const dd_cache* cache, int32_t S, int32_t T, int32_t n_heads,
                                           int32_t max_new, int32_t max_kv);
