@@ -74,7 +74,8 @@ typedef enum { DD_NORM_LAYER = 0, DD_NORM_RMS = 1 } dd_norm;
                               logit where one is needed); that row's output is a fallback:
                               z_s = z_t (posterior), z = 0 (verification) */
 #define DD_DEVERR_CACHE 8  /* cached context: a length, a block number or a row map does not fit (see
-                              dd_cache_plan, dd_cache_append, dd_cache_attention) */
+                              dd_cache_plan, dd_cache_append, dd_cache_attention, dd_cache_fork) */
+#define DD_DEVERR_SAMPLING 16 /* a sampling setting or a row number is out of range (see dd_token_sample) */
 
 /*
  * Denoiser architecture.  Pre-LN transformer, bidirectional attention (other
@@ -530,7 +531,8 @@ typedef struct {
  * length comes to the host).
  *   seq_len      [S] tokens that sequence s has in the cache and keeps (after a verification: those before
  *                the pass plus those accepted; what stands behind them is written over)
- *   n_new        [S] tokens it adds in this pass, >= 0; -1 ends the sequence and gives its blocks back
+ *   n_new        [S] tokens it adds in this pass, >= 0; -1 ends the sequence and gives its blocks back (one that shares
+ *                blocks with others ends by dd_cache_fork)
  *   held         [S] blocks it holds now; may be map->held itself
  *   free_blocks  [n_blocks] a stack: its first *n_free entries are the blocks nobody holds.  Ended
  *                sequences' blocks are pushed first, in the order of sequences and table entries, then
@@ -665,6 +667,123 @@ dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, i
                          void* out, int32_t rows_per_seq, const dd_logits_edits* edits, int32_t* dev_err,
                          void* stream);
 
+/* ---------------------------------------------------------------- tokens under settings */
+
+/*
+ * Which classes of a row of logits stay, per sequence (device arrays; NULL: without).  Classes are in order by falling
+ * logit l, the lowest index first among equal ones (-0 is 0), those of -inf left out; w = exp((l - max) / temperature).
+ * What stays is a beginning of that order:
+ *   min-p  the classes of w >= min_p;
+ *   top-k  the first top_k of those;
+ *   top-p  the shortest beginning of those whose weights add up to top_p times their sum or more, one class at least.
+ */
+typedef struct {
+    const float* temperature;   /* finite, >= 0; 0: the first class alone.  NULL: 1 */
+    const int32_t* top_k;       /* <= 0: without */
+    const float* top_p;         /* >= 0; >= 1: without */
+    const float* min_p;         /* in [0, 1]; 0: without */
+} dd_sampling;
+
+/*
+ * dd_token_sample - a token per draw: the first class in the order above at which the running sum of the weights exceeds u times
+ * the sum of what stays.
+ *   logits       device [rows][ld] of logits_dtype, finite or -inf, one finite at least per row read; ld >= V, ld % 8 == 0,
+ *                16-byte aligned
+ *   row_ids      device int32 [n], row of each draw (a pass's last row of each sequence; one row for several draws), -1: no draw,
+ *                its outputs are left as they were; other numbers outside [0, rows) set DD_DEVERR_SAMPLING and count as -1.
+ *                NULL: draw i reads row i (n <= rows)
+ *   draws_per_seq  draw i takes the settings of entry i / draws_per_seq, ceil(n / draws_per_seq) entries
+ *   noise_words  device uint32 [n]; NULL: Philox under `seed`, draw i the word (0, row0 + i, step, 6).  A word w stands for
+ *                u = (w + 1/2) 2^-32
+ *   z_out        device int32 [n]
+ *   logp         NULL or device fp32 [n]: log of the token's share of the weights that stay
+ *   n_kept       NULL or device int32 [n]: how many classes stay
+ *   dev_err      NULL or device int32 error word.  A row that allows no draw (NaN, +inf, no finite logit) sets
+ *                DD_DEVERR_LOGITS, a setting outside its range DD_DEVERR_SAMPLING; such a draw gives token 0, a NaN logp and
+ *                n_kept 0.
+ * Arithmetic: exponentials in 64 bits, rounded to multiples of 2^-46 (V > 65536: 2^(ceil(log2 V) - 62)) and summed as whole
+ * numbers, so results do not depend on the order of any sum.
+ */
+dd_status dd_token_sample(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V,
+                          const int32_t* row_ids, int32_t n, int32_t draws_per_seq, const dd_sampling* how,
+                          const uint32_t* noise_words, uint64_t seed, uint32_t step, uint32_t row0, int32_t* z_out,
+                          float* logp, int32_t* n_kept, int32_t* dev_err, void* stream);
+
+/*
+ * dd_logits_truncate - the same choice as an edit: out = l / temperature (l where that is 0) for the classes that stay, in
+ * fp32, held within the type's finite numbers and rounded once, -inf for the others.  dd_posterior_sample and dd_spec_verify then draw from the
+ * distribution that dd_token_sample draws from (truncate p and q alike, and the verified tokens follow the truncated target).
+ *   out          device [rows][ld]; may be logits itself, or must not overlap it; columns >= V are left untouched
+ *   Row m takes the settings of entry m / rows_per_seq.  A row that allows no choice (dd_token_sample) goes through as it is.
+ * Other arguments and errors as dd_token_sample.
+ */
+dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V, void* out,
+                             int32_t rows_per_seq, const dd_sampling* how, int32_t* n_kept, int32_t* dev_err,
+                             void* stream);
+
+/* ---------------------------------------------------------------- contexts that go on in several sequences */
+
+/*
+ * dd_cache_fork - the sequences of the next passes from those that there are: each takes the first tokens of some sequence's
+ * context (several continuations of a prompt, candidates chosen anew, requests that end).  Whole blocks are shared, no
+ * key or value is copied here; a partly filled last block belongs to one sequence alone, since that appends into it.
+ *   map          the old sequences: S, ld_table, block_table, held, kv_len (its row arrays are not looked at); S <= 2^16
+ *   to           the new ones, S and ld_table of their own; block_table, held and kv_len are written and overlap no array of
+ *                the old ones.  Entries beyond a sequence's own are left as they were.
+ *   seq_len      [map->S] tokens that each old sequence has, at most held * P (map->kv_len after a pass)
+ *   src          [to->S] old sequence that new sequence s goes on from; -1: none, its held and kv_len become 0
+ *   keep         [to->S] tokens of it that s keeps, 0 <= keep <= seq_len[src]; not looked at where src is -1.
+ *                NULL: all of them
+ *   Row s of the new table is the first ceil(keep / P) entries of the old row src_s; held and kv_len say so.  Where that leaves
+ *   a last block partly filled, and another new sequence holds the block too, it stays with one that holds it whole, else with
+ *   the first of those whose last block it is; each of the others takes a fresh block in its place.
+ *   free_blocks, n_free, n_free_out  the stack as in dd_cache_plan: the blocks that the old sequences held and no new one holds
+ *                are pushed in ascending order, then the fresh ones are taken from the top in the order of sequences
+ *   moves        [to->S][2]: (block, fresh block) for each fresh one in that order, for dd_cache_copy, which has to run before
+ *                anything is appended; n_moves [1] their number
+ *   ws           >= dd_cache_fork_workspace_bytes, 256-byte aligned; shared by no two calls that can overlap
+ *   dev_err      NULL or device int32 error word
+ * The call does all of this or, where something does not fit, nothing: then DD_DEVERR_CACHE is set, the new sequences hold
+ * nothing (held and kv_len 0), n_free_out takes *n_free and n_moves 0; the old ones stay as they are.  That is so where the pool has too few
+ * blocks, a row would pass to->ld_table entries, or an input is no fork's (a length, count, sequence or block number out
+ * of range).  A block number outside [0, n_blocks) in the stack sets DD_DEVERR_CACHE.
+ * While sequences share blocks, they end by dd_cache_fork (src -1 or not chosen), not by dd_cache_plan's n_new = -1, which
+ * would give a shared block back under the others; and a sequence that goes back behind its `keep` tokens does so by
+ * dd_cache_fork with a smaller keep.
+ */
+size_t dd_cache_fork_workspace_bytes(const dd_cache* cache, int32_t S, int32_t S_to);
+dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd_cache_map* to, const int32_t* seq_len,
+                        const int32_t* src, const int32_t* keep, int32_t* free_blocks, const int32_t* n_free,
+                        int32_t* n_free_out, int32_t* moves, int32_t* n_moves, void* ws, size_t ws_bytes,
+                        int32_t* dev_err, void* stream);
+
+/*
+ * dd_cache_compact - the blocks in use to the lowest numbers of the pool, so that it can shrink.  With n blocks in use, the i-th
+ * of them that is n or more moves to the i-th number below n that is not in use.
+ *   map          S, ld_table, block_table and held are read; S <= 2^16
+ *   block_table_out  [S][ld_table], may be map->block_table: the tables under the new numbers, held entries alone
+ *   free_blocks  [n_blocks] is written anew: n_blocks - n entries, the lowest number on top; n_free_out [1] their number
+ *   moves        [n_blocks / 2][2]: (old number, new number), ascending, for dd_cache_copy; n_moves [1] their number
+ *   ws           >= dd_cache_compact_workspace_bytes, 256-byte aligned; shared by no two calls that can overlap
+ * Where a count or a block number of the tables is out of range, DD_DEVERR_CACHE is set, the held entries are passed on as they are, n_moves
+ * is 0, and free_blocks and n_free_out are left as they were.
+ */
+size_t dd_cache_compact_workspace_bytes(const dd_cache* cache);
+dd_status dd_cache_compact(const dd_cache* cache, const dd_cache_map* map, int32_t* block_table_out, int32_t* free_blocks,
+                           int32_t* n_free_out, int32_t* moves, int32_t* n_moves, void* ws, size_t ws_bytes,
+                           int32_t* dev_err, void* stream);
+
+/*
+ * dd_cache_copy - blocks of the cache in every layer: codes and scales of block moves[i][0] into block moves[i][1], for
+ * i < min(*n_moves, max_moves).
+ *   codes, scales  the cache of every layer in turn, [n_layers] of what dd_cache describes
+ *   moves        device int32 [max_moves][2]; no block that is written is read or written by another move.  A block number
+ *                outside [0, n_blocks) sets DD_DEVERR_CACHE and its move is left out.
+ *   n_moves      device int32 [1]
+ */
+dd_status dd_cache_copy(const dd_cache* cache, void* codes, float* scales, int32_t n_layers, const int32_t* moves,
+                        const int32_t* n_moves, int32_t max_moves, int32_t* dev_err, void* stream);
+
 /* ---------------------------------------------------------------- profiling */
 
 /*
@@ -678,7 +797,8 @@ dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, i
  * Classes: 0 time_embedding, 1 embed_layernorm, 2 layernorm, 3 gemm_qkv,
  * 4 attention, 5 gemm_attn_out, 6 gemm_mlp_up, 7 gemm_mlp_down, 8 gemm_vocab,
  * 9 posterior_sample, 10 gaussian_latent, 11 init_params, 12 copy, 13 compact_masked,
- * 14 gemm_lora_down, 15 cache_plan, 16 cache_append, 17 cache_attention, 18 logits_edit.
+ * 14 gemm_lora_down, 15 cache_plan, 16 cache_append, 17 cache_attention, 18 logits_edit, 19 token_sample,
+ * 20 logits_truncate, 21 cache_fork, 22 cache_copy, 23 cache_compact.
  */
 dd_status dd_profile_begin(int32_t max_launches, uint32_t class_mask);
 dd_status dd_profile_end(void);

@@ -24,6 +24,7 @@ DD_DEVERR_TOKEN = 1
 DD_DEVERR_MASK = 2
 DD_DEVERR_LOGITS = 4
 DD_DEVERR_CACHE = 8
+DD_DEVERR_SAMPLING = 16
 DD_LOOP_POSTERIOR_PASS = 1
 DD_LOOP_STORE_FREE = 2
 ATTN_PATTERNS = {"bidirectional": 0, "causal": 1, "block_causal": 2, "draft_train": 3}
@@ -40,7 +41,8 @@ EXPORTED = [
     "dd_gaussian_latent_argmax", "dd_spec_verify_workspace_bytes", "dd_spec_verify_noise_width",
     "dd_spec_verify", "dd_spec_verify_noalloc", "dd_cache_plan", "dd_cache_append",
     "dd_cache_attention_workspace_bytes", "dd_cache_attention", "dd_logits_edit", "dd_cached_workspace_bytes",
-    "dd_denoise_forward_cached", "dd_profile_begin",
+    "dd_denoise_forward_cached", "dd_token_sample", "dd_logits_truncate", "dd_cache_fork_workspace_bytes",
+    "dd_cache_fork", "dd_cache_compact_workspace_bytes", "dd_cache_compact", "dd_cache_copy", "dd_profile_begin",
     "dd_profile_end", "dd_profile_num_classes", "dd_profile_read",
 ]
 
@@ -79,6 +81,11 @@ class DDLogitsEdits(ctypes.Structure):
                 ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
                 ("allow", ctypes.c_void_p), ("ld_allow", ctypes.c_int64), ("n_allow", ctypes.c_int32),
                 ("allow_id", ctypes.c_void_p)]
+
+
+class DDSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
 
 
 class DDError(RuntimeError):
@@ -154,6 +161,15 @@ def lib():
                                                       c.c_int32, P, P, c.c_int64, P, c.c_size_t, P]),
             "dd_logits_edit": (c.c_int32, [P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, P, c.c_int32,
                                            c.POINTER(DDLogitsEdits), P, P]),
+            "dd_token_sample": (c.c_int32, [P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, P, c.c_int32, c.c_int32,
+                                            c.POINTER(DDSampling), P, c.c_uint64, c.c_uint32, c.c_uint32, P, P, P, P, P]),
+            "dd_logits_truncate": (c.c_int32, [P, c.c_int32, c.c_int64, c.c_int32, c.c_int32, P, c.c_int32,
+                                               c.POINTER(DDSampling), P, P, P]),
+            "dd_cache_fork_workspace_bytes": (c.c_size_t, [cachep, c.c_int32, c.c_int32]),
+            "dd_cache_fork": (c.c_int32, [cachep, mapp, mapp, P, P, P, P, P, P, P, P, P, c.c_size_t, P, P]),
+            "dd_cache_compact_workspace_bytes": (c.c_size_t, [cachep]),
+            "dd_cache_compact": (c.c_int32, [cachep, mapp, P, P, P, P, P, P, c.c_size_t, P, P]),
+            "dd_cache_copy": (c.c_int32, [cachep, P, P, c.c_int32, P, P, c.c_int32, P, P]),
             "dd_profile_begin": (c.c_int32, [c.c_int32, c.c_uint32]),
             "dd_profile_end": (c.c_int32, []),
             "dd_profile_num_classes": (c.c_int32, []),
@@ -686,6 +702,84 @@ def logits_edit(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, history=
         rows_per_seq, ctypes.byref(e), _dev(dev_err, dev, 1, "dev_err", i32), stream))
 
 
+def _sampling(dev, entries, temperature, top_k, top_p, min_p):
+    torch = _torch()
+    f32 = torch.float32
+    return DDSampling(_dev(temperature, dev, entries, "temperature", f32), _dev(top_k, dev, entries, "top_k", torch.int32),
+                      _dev(top_p, dev, entries, "top_p", f32), _dev(min_p, dev, entries, "min_p", f32))
+
+
+def token_sample(logits, logits_dtype, ld, rows, V, z_out, n, row_ids=None, draws_per_seq=1, temperature=None, top_k=None,
+                 top_p=None, min_p=None, noise_words=None, seed=0, step=0, row0=0, logp=None, n_kept=None, dev_err=None):
+    """dd_token_sample: n draws, draw i from row row_ids[i] (or i) under the settings of entry i // draws_per_seq."""
+    torch = _torch()
+    i32 = torch.int32
+    dev, stream = _current()
+    how = _sampling(dev, -(-n // draws_per_seq) if draws_per_seq > 0 else 0, temperature, top_k, top_p, min_p)
+    _check(lib().dd_token_sample(
+        _dev(logits, dev, rows * ld, "logits", torch.bfloat16 if logits_dtype == "bf16" else torch.float32),
+        dtype_code(logits_dtype), ld, rows, V, _dev(row_ids, dev, n, "row_ids", i32), n, draws_per_seq, ctypes.byref(how),
+        _dev(noise_words, dev, n, "noise_words", i32), seed & 0xFFFFFFFFFFFFFFFF, step, row0, _dev(z_out, dev, n, "z_out", i32),
+        _dev(logp, dev, n, "logp", torch.float32), _dev(n_kept, dev, n, "n_kept", i32), _dev(dev_err, dev, 1, "dev_err", i32),
+        stream))
+
+
+def logits_truncate(logits, logits_dtype, ld, rows, V, out, rows_per_seq=1, temperature=None, top_k=None, top_p=None,
+                    min_p=None, n_kept=None, dev_err=None):
+    """dd_logits_truncate; row m takes the settings of entry m // rows_per_seq."""
+    torch = _torch()
+    i32 = torch.int32
+    t = torch.bfloat16 if logits_dtype == "bf16" else torch.float32
+    dev, stream = _current()
+    how = _sampling(dev, -(-rows // rows_per_seq) if rows_per_seq > 0 else 0, temperature, top_k, top_p, min_p)
+    _check(lib().dd_logits_truncate(
+        _dev(logits, dev, rows * ld, "logits", t), dtype_code(logits_dtype), ld, rows, V, _dev(out, dev, rows * ld, "out", t),
+        rows_per_seq, ctypes.byref(how), _dev(n_kept, dev, rows, "n_kept", i32), _dev(dev_err, dev, 1, "dev_err", i32), stream))
+
+
+def cache_fork_workspace_bytes(cc, S, S_to):
+    return int(lib().dd_cache_fork_workspace_bytes(ctypes.byref(cc), int(S), int(S_to)))
+
+
+def cache_fork(cc, m, to, seq_len, src, free_blocks, n_free, n_free_out, moves, n_moves, ws, keep=None, dev_err=None):
+    """dd_cache_fork: the sequences of the CacheMap `to` from those of `m`; moves is [to.S, 2]."""
+    i32 = _torch().int32
+    dev, stream = _current()
+    _check(lib().dd_cache_fork(
+        ctypes.byref(cc), m.on(dev), to.on(dev), _dev(seq_len, dev, m.S, "seq_len", i32), _dev(src, dev, to.S, "src", i32),
+        _dev(keep, dev, to.S, "keep", i32), _dev(free_blocks, dev, cc.n_blocks, "free_blocks", i32),
+        _dev(n_free, dev, 1, "n_free", i32), _dev(n_free_out, dev, 1, "n_free_out", i32), _dev(moves, dev, 2 * to.S, "moves", i32),
+        _dev(n_moves, dev, 1, "n_moves", i32), _dev(ws, dev, 0, "ws", ws.dtype), ws.numel() * ws.element_size(),
+        _dev(dev_err, dev, 1, "dev_err", i32), stream))
+
+
+def cache_compact_workspace_bytes(cc):
+    return int(lib().dd_cache_compact_workspace_bytes(ctypes.byref(cc)))
+
+
+def cache_compact(cc, m, block_table_out, free_blocks, n_free_out, moves, n_moves, ws, dev_err=None):
+    """dd_cache_compact; block_table_out may be m.block_table, moves is [n_blocks // 2 or more, 2]."""
+    i32 = _torch().int32
+    dev, stream = _current()
+    _check(lib().dd_cache_compact(
+        ctypes.byref(cc), m.on(dev), _dev(block_table_out, dev, m.S * m.ld_table, "block_table_out", i32),
+        _dev(free_blocks, dev, cc.n_blocks, "free_blocks", i32), _dev(n_free_out, dev, 1, "n_free_out", i32),
+        _dev(moves, dev, cc.n_blocks // 2 * 2, "moves", i32), _dev(n_moves, dev, 1, "n_moves", i32), _dev(ws, dev, 0, "ws", ws.dtype),
+        ws.numel() * ws.element_size(), _dev(dev_err, dev, 1, "dev_err", i32), stream))
+
+
+def cache_copy(cc, codes, scales, moves, n_moves, layers=1, dev_err=None):
+    """dd_cache_copy over the caches of `layers` layers; moves is [max_moves, 2]."""
+    i32 = _torch().int32
+    dev, stream = _current()
+    _two_dims(moves, "moves")
+    if moves.shape[1] != 2:
+        raise ValueError(f"moves must be [max_moves, 2], got {tuple(moves.shape)}")
+    pc, ps = _cache_ptrs(cc, dev, codes, scales, layers)
+    _check(lib().dd_cache_copy(ctypes.byref(cc), pc, ps, layers, _dev(moves, dev, 0, "moves", i32),
+                               _dev(n_moves, dev, 1, "n_moves", i32), moves.shape[0], _dev(dev_err, dev, 1, "dev_err", i32), stream))
+
+
 def _two_dims(t, name):
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
@@ -706,7 +800,8 @@ def read_device_error(err):
 PROFILE_CLASSES = ["time_embedding", "embed_layernorm", "layernorm", "gemm_qkv", "attention",
                    "gemm_attn_out", "gemm_mlp_up", "gemm_mlp_down", "gemm_vocab",
                    "posterior_sample", "gaussian_latent", "init_params", "copy", "compact_masked",
-                   "gemm_lora_down", "cache_plan", "cache_append", "cache_attention", "logits_edit"]
+                   "gemm_lora_down", "cache_plan", "cache_append", "cache_attention", "logits_edit",
+                   "token_sample", "logits_truncate", "cache_fork", "cache_copy", "cache_compact"]
 
 
 def profile_begin(max_launches, classes=None):

@@ -16,7 +16,8 @@ LIB = os.path.join(PKG, "libdd.so")
 
 SOURCES = ["dd_api.hip", "k_posterior.hip", "k_latent_init.hip", "k_norm.hip", "k_gemm.hip",
            "k_gemm_ring.hip",
-           "k_attn.hip", "k_verify.hip", "k_cache.hip", "k_cache_attn.hip", "k_edit.hip"]
+           "k_attn.hip", "k_verify.hip", "k_cache.hip", "k_cache_attn.hip", "k_edit.hip",
+           "k_sample.hip", "k_pages.hip"]
 
 # Per-file extra flags.  Attention keeps its MFMA accumulators in ordinary VGPRs (the softmax reads
 # every score with VALU instructions; AGPR accumulators would need a copy per score).  The GEMMs need

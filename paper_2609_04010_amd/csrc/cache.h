@@ -92,6 +92,50 @@ struct CacheAttnPlan {
 CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int dh, int32_t max_new, int32_t max_kv);
 dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
+// Ranges of blocks that a fork or a compaction cuts the pool into (n_blocks is below 2^26).
+constexpr int PAGE_RANGE = 8192, PAGE_RANGES = (1 << 26) / PAGE_RANGE;
+
+struct ForkArgs {
+    CacheShape c;
+    int32_t S, S_to, ld_table, ld_to;
+    const int32_t *table, *held, *seq_len, *src, *keep;
+    int32_t *to_table, *to_held, *to_len;
+    int32_t* free_blocks;
+    const int32_t* n_free;
+    int32_t *n_free_out, *moves, *n_moves;
+    // workspace: a bit per block that is freed, their number in each range, whether a sequence takes a fresh block, whether
+    // an input is no fork's
+    uint32_t* freed;
+    int32_t *counts, *copies, *bad;
+    int32_t ranges;
+    int32_t* err;
+};
+dd_status launch_cache_fork(const ForkArgs& a, hipStream_t s);
+
+struct CompactArgs {
+    CacheShape c;
+    int32_t S, ld_table;
+    const int32_t *table, *held;
+    int32_t *to_table, *free_blocks, *n_free_out, *moves, *n_moves;
+    // workspace: a bit per block in use, those of the range before each word of them, those of each range, whether an
+    // input is no table
+    uint32_t* used;
+    int32_t *before, *counts, *bad;
+    int32_t ranges;
+    int32_t* err;
+};
+dd_status launch_cache_compact(const CompactArgs& a, hipStream_t s);
+
+struct CopyArgs {
+    int32_t n_blocks, heads, layers, max_moves;
+    int64_t slab;        // bytes of a block's codes
+    uint8_t* codes;
+    float* scales;
+    const int32_t *moves, *n_moves;
+    int32_t* err;
+};
+dd_status launch_cache_copy(const CopyArgs& a, hipStream_t s);
+
 struct EditArgs {
     const void* logits;
     void* out;

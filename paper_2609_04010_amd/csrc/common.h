@@ -93,6 +93,7 @@ enum KernelClass {
     KC_TEMB = 0, KC_EMBED_LN, KC_LN, KC_GEMM_QKV, KC_ATTN, KC_GEMM_O, KC_GEMM_MLP1,
     KC_GEMM_MLP2, KC_GEMM_VOCAB, KC_POSTERIOR, KC_LATENT, KC_INIT, KC_COPY, KC_COMPACT, KC_GEMM_LORA,
     KC_CACHE_PLAN, KC_CACHE_APPEND, KC_CACHE_ATTN, KC_LOGITS_EDIT,
+    KC_TOKEN_SAMPLE, KC_LOGITS_TRUNCATE, KC_CACHE_FORK, KC_CACHE_COPY, KC_CACHE_COMPACT,
     KC_COUNT
 };
 // A scope around one kernel launch (kernel = true) hands its event pair to that launch (launch_k),

@@ -56,7 +56,8 @@ static const char* kClassNames[KC_COUNT] = {
     "time_embedding", "embed_layernorm", "layernorm", "gemm_qkv", "attention", "gemm_attn_out",
     "gemm_mlp_up", "gemm_mlp_down", "gemm_vocab", "posterior_sample", "gaussian_latent",
     "init_params", "copy", "compact_masked", "gemm_lora_down", "cache_plan",
-    "cache_append", "cache_attention", "logits_edit"};
+    "cache_append", "cache_attention", "logits_edit", "token_sample", "logits_truncate",
+    "cache_fork", "cache_copy", "cache_compact"};
 
 // The recorder is the library's only process-wide mutable state: guarded by g_prof_mu, and skipped
 // without taking the lock while it is off.
@@ -1079,6 +1080,137 @@ dd_status dd_logits_edit(const void* logits, int32_t logits_dtype, int64_t ld, i
     EditArgs a = {logits, out, ld, rows, V, rows_per_seq, *edits, 0, dev_err};
     if (!a.e.history) a.e.ld_history = 0;
     return launch_edit(a, logits_dtype, (hipStream_t)stream);
+}
+
+// Checks shared by dd_token_sample and dd_logits_truncate.
+static dd_status sampling_check(int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V, int32_t per,
+                                const dd_sampling* how) {
+    DD_CHECK(logits_dtype == DD_BF16 || logits_dtype == DD_FP32, DD_E_DTYPE, "unknown logits dtype");
+    DD_CHECK(rows >= 0 && V > 0 && per > 0, DD_E_ARG, "rows must be >= 0, V and the rows or draws per sequence > 0");
+    DD_CHECK(V <= (1 << 24) && rows <= (1 << 30), DD_E_UNSUPPORTED, "V > 2^24 or rows > 2^30 unsupported");
+    DD_CHECK(ld >= V && ld % 8 == 0, DD_E_SHAPE, "ld must be >= V and a multiple of 8");
+    DD_CHECK(how, DD_E_ARG, "how is NULL");
+    return DD_OK;
+}
+
+dd_status dd_token_sample(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V,
+                          const int32_t* row_ids, int32_t n, int32_t draws_per_seq, const dd_sampling* how,
+                          const uint32_t* noise_words, uint64_t seed, uint32_t step, uint32_t row0, int32_t* z_out,
+                          float* logp, int32_t* n_kept, int32_t* dev_err, void* stream) {
+    DD_TRY(sampling_check(logits_dtype, ld, rows, V, draws_per_seq, how));
+    DD_CHECK(n >= 0 && n <= (1 << 30), DD_E_ARG, "n must lie in [0, 2^30]");
+    DD_CHECK(row_ids || n <= rows, DD_E_SHAPE, "%d draws of %d rows need row_ids", n, rows);
+    if (n == 0) return DD_OK;
+    DD_CHECK(z_out && (logits || rows == 0), DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(((uintptr_t)logits & 15) == 0, DD_E_ARG, "logits must be 16-byte aligned");
+    SampleArgs a = {logits, ld, rows, V, row_ids, n, draws_per_seq, how->temperature, how->top_k, how->top_p, how->min_p,
+                    noise_words, seed, step, row0, z_out, logp, nullptr, n_kept, dev_err, 0};
+    return launch_sample(a, logits_dtype, true, (hipStream_t)stream);
+}
+
+dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t ld, int32_t rows, int32_t V, void* out,
+                             int32_t rows_per_seq, const dd_sampling* how, int32_t* n_kept, int32_t* dev_err,
+                             void* stream) {
+    DD_TRY(sampling_check(logits_dtype, ld, rows, V, rows_per_seq, how));
+    if (rows == 0) return DD_OK;
+    DD_CHECK(logits && out, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK((((uintptr_t)logits | (uintptr_t)out) & 15) == 0, DD_E_ARG, "logits and out must be 16-byte aligned");
+    SampleArgs a = {logits, ld, rows, V, nullptr, rows, rows_per_seq, how->temperature, how->top_k, how->top_p, how->min_p,
+                    nullptr, 0, 0, 0, nullptr, nullptr, out, n_kept, dev_err, 0};
+    return launch_sample(a, logits_dtype, false, (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- blocks between passes
+
+struct PageWs {
+    size_t bits, before, counts, copies, total;
+    int32_t ranges;
+};
+static PageWs page_ws(const dd_cache* c, int64_t copies, bool before) {
+    PageWs w;
+    w.ranges = (int32_t)ceil_div(c->n_blocks, PAGE_RANGE);
+    const size_t words = align256(4 * (size_t)ceil_div(c->n_blocks, 32));
+    w.bits = 256;                       // (the first word says whether an input does not fit)
+    w.before = w.bits + words;
+    w.counts = w.before + (before ? words : 0);
+    w.copies = w.counts + align256(4 * (size_t)w.ranges);
+    w.total = w.copies + align256(4 * (size_t)copies);
+    return w;
+}
+
+// Checks of a table that a fork or a compaction reads or writes.
+static dd_status pages_map_check(const dd_cache* cache, const dd_cache_map* m) {
+    DD_TRY(cache_check(cache));
+    DD_CHECK(m, DD_E_ARG, "map is NULL");
+    DD_CHECK(m->S >= 0 && m->ld_table >= 1, DD_E_ARG, "S must not be negative, ld_table positive");
+    DD_CHECK(m->S <= (1 << 16) && m->ld_table <= (1 << 26), DD_E_UNSUPPORTED,
+             "more than 2^16 sequences or 2^26 blocks per sequence unsupported");
+    DD_CHECK(m->S == 0 || (m->block_table && m->held && m->kv_len), DD_E_ARG, "NULL pointer argument");
+    return DD_OK;
+}
+
+size_t dd_cache_fork_workspace_bytes(const dd_cache* cache, int32_t S, int32_t S_to) {
+    if (cache_check(cache) != DD_OK || S < 0 || S > (1 << 16) || S_to < 0 || S_to > (1 << 16)) return 0;
+    return page_ws(cache, S_to, false).total;
+}
+
+dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd_cache_map* to, const int32_t* seq_len,
+                        const int32_t* src, const int32_t* keep, int32_t* free_blocks, const int32_t* n_free,
+                        int32_t* n_free_out, int32_t* moves, int32_t* n_moves, void* ws, size_t ws_bytes,
+                        int32_t* dev_err, void* stream) {
+    DD_TRY(pages_map_check(cache, map));
+    DD_TRY(pages_map_check(cache, to));
+    DD_CHECK(map->S == 0 || seq_len, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(to->S == 0 || (src && moves), DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(free_blocks && n_free && n_free_out && n_moves, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(map->S == 0 || to->S == 0 || (map->block_table != to->block_table && map->held != to->held &&
+                                           map->kv_len != to->kv_len && seq_len != to->kv_len),
+             DD_E_ARG, "the new tables and lengths must be other arrays than the old ones");
+    const PageWs w = page_ws(cache, to->S, false);
+    DD_CHECK(ws && ((uintptr_t)ws & 255) == 0, DD_E_ARG, "ws must be a 256-byte aligned buffer");
+    DD_CHECK(ws_bytes >= w.total, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, w.total);
+    char* b = (char*)ws;
+    ForkArgs a = {cache_shape(cache), map->S, to->S, map->ld_table, to->ld_table, map->block_table, map->held, seq_len, src,
+                  keep, to->block_table, to->held, to->kv_len, free_blocks, n_free, n_free_out, moves, n_moves,
+                  (uint32_t*)(b + w.bits), (int32_t*)(b + w.counts), (int32_t*)(b + w.copies), (int32_t*)b, w.ranges, dev_err};
+    return launch_cache_fork(a, (hipStream_t)stream);
+}
+
+size_t dd_cache_compact_workspace_bytes(const dd_cache* cache) {
+    if (cache_check(cache) != DD_OK) return 0;
+    return page_ws(cache, 0, true).total;
+}
+
+dd_status dd_cache_compact(const dd_cache* cache, const dd_cache_map* map, int32_t* block_table_out, int32_t* free_blocks,
+                           int32_t* n_free_out, int32_t* moves, int32_t* n_moves, void* ws, size_t ws_bytes,
+                           int32_t* dev_err, void* stream) {
+    DD_TRY(pages_map_check(cache, map));
+    DD_CHECK((map->S == 0 || block_table_out) && free_blocks && n_free_out && n_moves && (moves || cache->n_blocks == 1),
+             DD_E_ARG, "NULL pointer argument");
+    const PageWs w = page_ws(cache, 0, true);
+    DD_CHECK(ws && ((uintptr_t)ws & 255) == 0, DD_E_ARG, "ws must be a 256-byte aligned buffer");
+    DD_CHECK(ws_bytes >= w.total, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, w.total);
+    char* b = (char*)ws;
+    CompactArgs a = {cache_shape(cache), map->S, map->ld_table, map->block_table, map->held, block_table_out, free_blocks,
+                     n_free_out, moves, n_moves, (uint32_t*)(b + w.bits), (int32_t*)(b + w.before), (int32_t*)(b + w.counts),
+                     (int32_t*)b, w.ranges, dev_err};
+    return launch_cache_compact(a, (hipStream_t)stream);
+}
+
+dd_status dd_cache_copy(const dd_cache* cache, void* codes, float* scales, int32_t n_layers, const int32_t* moves,
+                        const int32_t* n_moves, int32_t max_moves, int32_t* dev_err, void* stream) {
+    DD_TRY(cache_check(cache));
+    DD_CHECK(n_layers >= 0 && max_moves >= 0, DD_E_ARG, "n_layers and max_moves must not be negative");
+    const int64_t slab = 2 * (int64_t)cache->n_kv_heads * cache->block * cache->head_dim;
+    DD_CHECK(n_layers <= (1 << 16) && slab * n_layers <= ((int64_t)1 << 40), DD_E_UNSUPPORTED,
+             "more than 2^16 layers, or 2^40 bytes of a block in all layers, unsupported");
+    if (n_layers == 0 || max_moves == 0) return DD_OK;
+    DD_CHECK(codes && scales && moves && n_moves, DD_E_ARG, "NULL pointer argument");
+    DD_CHECK(((uintptr_t)codes & 15) == 0 && ((uintptr_t)scales & 7) == 0, DD_E_ARG,
+             "codes must be 16-byte aligned, scales 8-byte aligned");
+    CopyArgs a = {cache->n_blocks, cache->n_kv_heads, n_layers, max_moves, slab, (uint8_t*)codes, scales, moves, n_moves,
+                  dev_err};
+    return launch_cache_copy(a, (hipStream_t)stream);
 }
 
 dd_status dd_profile_begin(int32_t max_launches, uint32_t class_mask) {

@@ -155,6 +155,27 @@ dd_status launch_verify(const VerifyArgs& a, int logits_dtype, float* lse, hipSt
 // Device address of the current device's DD_SPEC_VERIFY_NOALLOC_ROWS-float array of
 // dd_spec_verify_noalloc (looked up on the first call on each device).
 dd_status verify_noalloc_scratch(float** out);
+
+// Tokens (draw) or rows with what stays, of n draws or rows; draw i takes entry i / per of the settings.
+struct SampleArgs {
+    const void* logits;
+    int64_t ld;
+    int32_t rows, V;
+    const int32_t* row_ids;   // draws: row of each, or NULL
+    int32_t n, per;
+    const float* temperature;
+    const int32_t* top_k;
+    const float *top_p, *min_p;
+    const uint32_t* noise;    // explicit words [n] or NULL (Philox)
+    uint64_t seed;
+    uint32_t step, row0;
+    int32_t* z;
+    float* logp;
+    void* out;
+    int32_t *kept, *err;
+    int frac;                 // set by launch_sample
+};
+dd_status launch_sample(const SampleArgs& a, int logits_dtype, bool draw, hipStream_t s);
 dd_status launch_latent(const int32_t* x, int32_t rows, int32_t V, double at, double sigma,
                         uint64_t seed, uint32_t step, uint32_t row0, int32_t* z, int32_t* err,
                         hipStream_t s);

@@ -18,7 +18,7 @@
 namespace dd {
 
 enum Stream : uint32_t { STREAM_TOP = 0, STREAM_CLASS = 1, STREAM_LATENT = 2, STREAM_PARAM = 3, STREAM_VERIFY = 4,
-                         STREAM_GROUP_U = 5 };
+                         STREAM_GROUP_U = 5, STREAM_TOKEN = 6 };
 
 struct Words4 {
     uint32_t w[4];
