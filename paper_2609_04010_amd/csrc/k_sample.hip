@@ -34,7 +34,7 @@ DD_DEV float key_value(uint32_t k) {
 // the place in the whole order
 DD_DEV uint64_t place(float l, int v) { return ((uint64_t)value_key(l) << 32) | (uint32_t)v; }
 
-constexpr int TAB = 256;     // 2^(-j / TAB)
+constexpr int TAB = 64;      // 2^(-j / TAB)
 constexpr int LIST = 64;     // classes of a bin that are ordered one by one
 
 template <int NT>
@@ -63,13 +63,28 @@ struct RowScale {
     bool weigh;              // sums of weights are needed
 };
 
+// 2^(-j / TAB), from its series (25 terms, each factor below ln 2)
+struct PowerTable {
+    double v[TAB];
+    constexpr PowerTable() : v() {
+        for (int j = 0; j < TAB; ++j) {
+            const double x = -0.69314718055994530942 * j / TAB;
+            double e = 1.0;
+            for (int n = 25; n > 0; --n) e = 1.0 + e * x / n;
+            v[j] = e;
+        }
+    }
+};
+__constant__ PowerTable power_table = PowerTable();
+
 // w 2^frac, rounded.  With t = turn (top - l) = n + f, |f| <= 1/2: w = 2^-(n / TAB) 2^(-f / TAB), the first factor from the
-// table and an exponent, the second from the first five terms of its series (the next is below 4e-17).
+// table and an exponent, the second from the first six terms of its series (the next is below 4e-17).
 DD_DEV uint64_t weight(const RowScale& s, const double* tab, float l) {
     const double t = fmin(s.turn * ((double)s.top - (double)l), 64.0 * TAB);
     const double n = rint(t), x = (n - t) * (0.69314718055994530942 / TAB);
     const int k = (int)n;
-    double e = fma(x, 1.0 / 24.0, 1.0 / 6.0);
+    double e = fma(x, 1.0 / 120.0, 1.0 / 24.0);
+    e = fma(x, e, 1.0 / 6.0);
     e = fma(x, e, 0.5);
     e = fma(x, e, 1.0);
     e = fma(x, e, 1.0);
@@ -139,7 +154,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
     __shared__ L sm;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int chunks = RES > 0 ? RES : (a.V + NT * E - 1) / (NT * E);
-    for (int j = tid; j < TAB; j += NT) sm.tab[j] = exp2(-(double)j / TAB);
+    if (tid < TAB) sm.tab[tid] = power_table.v[tid];
     for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
         int r = i;
         if (DRAW && a.row_ids) {
@@ -429,10 +444,582 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
     }
 }
 
+// ---------------------------------------------------------------- bf16 rows
+//
+// A bf16 number's 16 bits, as a signed whole number that orders like it (k = +-magnitude), are a bin of their own: equal
+// numbers are all that a bin holds, so a count gives its weight, the exponential is taken once per bin, and a bound
+// inside a bin is a division away.  A window of keys stands in LDS: MAGS magnitudes of either sign below the largest that can matter (weights
+// below e^-34 round to 0), with the numbers nearer to 0 in one bin between them, whose weights are summed one by one (few:
+// the window spans 16 binades).  Where a bound falls among those, or among numbers below the window (top-k alone can ask for
+// them), the next window is counted.  Two packed numbers are handled at a time.
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+
+constexpr int MAGS = 2047, ZERO = MAGS, KBINS = 2 * MAGS + 2;    // bins: positive, near 0, negative, one to spare
+constexpr int KMAX = 0x7F7F, KINF = 0x7F80;                      // keys of the largest number and of infinity
+
+DD_DEV s16x2 keys_of(uint32_t w) {
+    const s16x2 sign = __builtin_bit_cast(s16x2, w) >> (short)15;
+    const uint32_t m = (w & 0x7FFF7FFFu) ^ __builtin_bit_cast(uint32_t, sign);
+    return __builtin_bit_cast(s16x2, m) - sign;
+}
+DD_DEV float key_float(int k) { return __uint_as_float((uint32_t)(k < 0 ? 0x8000 - k : k) << 16); }
+
+// a value that all lanes have alike, where the compiler knows it; lane x's value
+DD_DEV int same(int v) { return __builtin_amdgcn_readfirstlane(v); }
+DD_DEV uint32_t same(uint32_t v) { return (uint32_t)same((int)v); }
+DD_DEV uint64_t same(uint64_t v) { return ((uint64_t)same((uint32_t)(v >> 32)) << 32) | same((uint32_t)v); }
+DD_DEV uint32_t of_lane(uint32_t v, int x) { return (uint32_t)__builtin_amdgcn_readlane((int)v, x); }
+DD_DEV uint64_t of_lane(uint64_t v, int x) { return ((uint64_t)of_lane((uint32_t)(v >> 32), x) << 32) | of_lane((uint32_t)v, x); }
+
+// inclusive prefix sums over the lanes: shifts within rows of 16, then the last lanes of rows into those behind them
+template <int CTRL, int ROWS> DD_DEV uint32_t moved(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true);
+}
+template <int CTRL, int ROWS> DD_DEV void scan_step(uint32_t& c, uint64_t& w) {
+    c += moved<CTRL, ROWS>(c);
+    w += ((uint64_t)moved<CTRL, ROWS>((uint32_t)(w >> 32)) << 32) | moved<CTRL, ROWS>((uint32_t)w);
+}
+DD_DEV void wave_scan(uint32_t& c, uint64_t& w) {
+    scan_step<0x111, 0xF>(c, w);
+    scan_step<0x112, 0xF>(c, w);
+    scan_step<0x114, 0xF>(c, w);
+    scan_step<0x118, 0xF>(c, w);
+    scan_step<0x142, 0xA>(c, w);
+    scan_step<0x143, 0xC>(c, w);
+}
+DD_DEV uint32_t wave_scan(uint32_t c) {
+    c += moved<0x111, 0xF>(c);
+    c += moved<0x112, 0xF>(c);
+    c += moved<0x114, 0xF>(c);
+    c += moved<0x118, 0xF>(c);
+    c += moved<0x142, 0xA>(c);
+    c += moved<0x143, 0xC>(c);
+    return c;
+}
+
+// The window that is counted: largest magnitude (the smallest is w_max - MAGS + 1), and the keys that count.
+struct Window {
+    int max, lo, hi;
+    DD_DEV int min() const { return max - MAGS + 1; }
+    DD_DEV int key(int bin) const { return bin < ZERO ? max - bin : bin == ZERO ? 0 : -(bin - ZERO - 1 + min()); }
+};
+
+template <int NT, int CH>
+struct KeyLds {
+    static constexpr int NW = NT / 64;
+    double tab[TAB];
+    uint32_t hist[KBINS + 64];       // counts; numbers outside the window go behind them, lane by lane
+    uint64_t pw[NT], tw[NW];         // weights of a thread's bins and those before them in its wavefront; of a wavefront's
+    uint32_t pc[NT], tc[NW];         // counts, likewise
+    int hi[NW], lo[NW];
+    uint64_t zero_w;
+    uint32_t zero_c, below;
+    uint32_t cell[CH * NW];          // equal numbers per chunk and wavefront
+    // what wavefront 0 decided: count this window (or, `ask`, the numbers below it), or the j-th of the numbers of key `last`
+    Window next;
+    int again, ask, last, pick, at;
+    uint32_t j;
+};
+
+template <int NT, int CH, bool DRAW>
+__global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys_kernel(SampleArgs a) {
+    using L = KeyLds<NT, CH>;
+    constexpr int NW = L::NW, BPT = KBINS / NT;
+    __shared__ __attribute__((aligned(16))) L sm;
+    const int tid = threadIdx.x, lane = tid & 63, wv = same(tid >> 6);
+    const int i = blockIdx.x;
+    int r = i;
+    if (DRAW && a.row_ids) {
+        r = a.row_ids[i];
+        if (r < 0 || r >= a.rows) {
+            if (r != -1 && tid == 0 && a.err) atomicOr(a.err, DD_DEVERR_SAMPLING);
+            return;
+        }
+    }
+    const bf16_t* row = (const bf16_t*)a.logits + (int64_t)r * a.ld;
+    s16x2 key[CH * 4];
+    {
+        uint4 u[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int v = (c * NT + tid) * 8;
+            u[c] = Elem<bf16_t>::NEG_INF4;
+            if (v < a.V) u[c] = *(const uint4*)(row + v);
+        }
+        if (tid < TAB) sm.tab[tid] = power_table.v[tid];
+#pragma unroll
+        for (int b = 0; b < BPT / 4; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int v = (c * NT + tid) * 8;
+            if (v < a.V && v + 8 > a.V) Elem<bf16_t>::clip(u[c], a.V - v);
+            key[4 * c] = keys_of(u[c].x);
+            key[4 * c + 1] = keys_of(u[c].y);
+            key[4 * c + 2] = keys_of(u[c].z);
+            key[4 * c + 3] = keys_of(u[c].w);
+        }
+    }
+    const int set = i / a.per;
+    const float t = a.temperature ? a.temperature[set] : 1.f, p = a.top_p ? a.top_p[set] : 1.f, m = a.min_p ? a.min_p[set] : 0.f;
+    const int k = a.top_k ? a.top_k[set] : 0;
+    // largest and smallest key (NaN stands beyond the infinities)
+    int kx, kn;
+    {
+        s16x2 x = key[0], n = key[0];
+#pragma unroll
+        for (int w = 1; w < CH * 4; ++w) {
+            x = __builtin_elementwise_max(x, key[w]);
+            n = __builtin_elementwise_min(n, key[w]);
+        }
+        kx = max((int)x[0], (int)x[1]);
+        kn = min((int)n[0], (int)n[1]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            kx = max(kx, __shfl_xor(kx, o, 64));
+            kn = min(kn, __shfl_xor(kn, o, 64));
+        }
+        if (lane == 0) {
+            sm.hi[wv] = kx;
+            sm.lo[wv] = kn;
+        }
+        if (tid == 0) {
+            sm.zero_c = sm.below = 0;
+            sm.zero_w = 0;
+        }
+        __syncthreads();
+        kx = sm.hi[lane & (NW - 1)];
+        kn = sm.lo[lane & (NW - 1)];
+#pragma unroll
+        for (int o = NW / 2; o > 0; o >>= 1) {
+            kx = max(kx, __shfl_xor(kx, o, 64));
+            kn = min(kn, __shfl_xor(kn, o, 64));
+        }
+        kx = same(kx);
+        kn = same(kn);
+    }
+    const bool settings = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f;   // (false for NaN)
+    if (kx >= KINF || kx <= -KINF || kn < -KINF || !settings) {
+        if (tid == 0) {
+            if (a.err) atomicOr(a.err, settings ? DD_DEVERR_LOGITS : DD_DEVERR_SAMPLING);
+            if (a.kept) a.kept[i] = 0;
+            if (DRAW) {
+                a.z[i] = 0;
+                if (a.logp) a.logp[i] = NAN;
+            }
+        }
+        if (!DRAW && a.out != a.logits) {
+            bf16_t* out = (bf16_t*)a.out + (int64_t)r * a.ld;
+            for (int v = tid; v < a.V; v += NT) out[v] = row[v];
+        }
+        return;
+    }
+    const float top = key_float(kx);
+    const RowScale q = {top, 0.f, 0.f, TAB * 1.4426950408889634 / (double)t, a.frac, DRAW || p < 1.f};
+    int kmin = -KMAX;            // the smallest key that min-p leaves
+    int mags;                    // the largest magnitude that can matter
+    {
+        float b = top - 34.f * t;
+        if (kn > -KINF) b = fmaxf(b, key_float(kn));
+        if (m > 0.f && t > 0.f) {          // w >= m where l >= top + t log m
+            const double e = (double)top + (double)t * log((double)m);
+            if (e > -FLT_MAX) {
+                float f = (float)e;
+                if ((double)f < e) f = key_value(value_key(f) - 1);    // the next number above
+                const uint32_t u = __float_as_uint(f);
+                kmin = same((int32_t)u < 0 ? -(int)((u & 0x7FFFFFFFu) >> 16) : (int)((u + 0xFFFFu) >> 16));
+                b = fmaxf(b, f);
+            }
+        }
+        mags = min(KMAX, (int)((__float_as_uint(b) & 0x7FFFFFFFu) >> 16) + 1);
+        mags = same(max(max(mags, kx < 0 ? -kx : kx), MAGS));
+    }
+    int last = kmin, pick = 0;           // key of the last that stays (or of the draw); whether the j-th of them is looked for
+    uint32_t j = 1, kept_c = 1;
+    uint64_t kept_w = 0;
+    if (t == 0.f || k == 1) {
+        last = kx;
+        pick = 1;
+    } else if (q.weigh || k > 0 || a.kept) {
+        Window win = {mags, kmin, KMAX};
+        // of wavefront 0: sums before the window; top-k, top-p and draw done; what is looked for
+        uint32_t base_c = 0, main_c = 0;
+        uint64_t base_w = 0, bound = 0;
+        int step = 0;
+        bool have = false, count = false, main = true;
+        int below = -1;                  // numbers below the main window, once they are counted
+        for (;;) {
+            // (what a pass makes of the keys is not to be kept for the next: there are too many)
+#pragma unroll
+            for (int x = 0; x < CH * 4; ++x) asm volatile("" : "+v"(key[x]));
+            {
+                const u16x2 hi = (u16x2)(unsigned short)win.max, mid = (u16x2)(unsigned short)ZERO;
+                const u16x2 sh = (u16x2)(unsigned short)(win.max + win.min() - (MAGS + 1)), out = (u16x2)(unsigned short)(KBINS + lane);
+#pragma unroll
+                for (int x = 0; x < CH * 4; ++x) {
+                    const u16x2 d = hi - __builtin_bit_cast(u16x2, key[x]);
+                    u16x2 b = __builtin_elementwise_min(d, __builtin_elementwise_max(mid, __builtin_elementwise_sub_sat(d, sh)));
+                    b = __builtin_elementwise_min(b, out);
+                    atomicAdd(&sm.hist[b[0]], 1u);
+                    atomicAdd(&sm.hist[b[1]], 1u);
+                }
+            }
+            __syncthreads();
+            const bool near = win.min() > 1 && same(sm.hist[ZERO]) != 0;       // (from magnitude 1 on, zeros are alone in their bin)
+            if (near) {
+#pragma unroll
+                for (int x = 0; x < CH * 4; ++x) asm volatile("" : "+v"(key[x]));
+                uint32_t zc = 0;
+                uint64_t zw = 0;
+                const int lo = max(win.lo, 1 - win.min()), hi = min(win.hi, win.min() - 1);
+                const u16x2 from = (u16x2)(unsigned short)(short)lo;
+#pragma unroll
+                for (int half = 0; half < CH; half += 8) {
+                    uint64_t some = 0;
+#pragma unroll
+                    for (int y = half; y < CH && y < half + 8; ++y) {
+                        u16x2 x = __builtin_bit_cast(u16x2, key[4 * y]) - from;
+#pragma unroll
+                        for (int z = 1; z < 4; ++z) x = __builtin_elementwise_min(x, __builtin_bit_cast(u16x2, key[4 * y + z]) - from);
+                        if (lo > hi || min(x[0], x[1]) > hi - lo) continue;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int f = key[4 * y + e / 2][e & 1];
+                            some |= (uint64_t)(f >= lo && f <= hi) << (8 * (y - half) + e);
+                        }
+                    }
+                    zc += __popcll(some);
+                    if (q.weigh)
+#pragma unroll 1
+                        for (; some; some &= some - 1) {
+                            const int x = __builtin_ctzll(some) + 8 * half;
+                            zw += weight(q, sm.tab, bf16_to_f32(row[((x >> 3) * NT + tid) * 8 + (x & 7)]));
+                        }
+                }
+                if (zc) {
+                    atomicAdd(&sm.zero_c, zc);
+                    atomicAdd((unsigned long long*)&sm.zero_w, (unsigned long long)zw);
+                }
+                __syncthreads();
+            }
+            // count and weight of a bin
+            auto bin_sums = [&](int bin, uint32_t n, uint32_t& c, uint64_t& w) {
+                const int f = win.key(bin);
+                c = f < win.lo || f > win.hi || bin == KBINS - 1 ? 0 : n;
+                w = c && q.weigh ? c * weight(q, sm.tab, key_float(f)) : 0;
+                if (near && bin == ZERO) {
+                    c = sm.zero_c;
+                    w = sm.zero_w;
+                }
+            };
+            uint32_t c_sum = 0;
+            uint64_t w_sum = 0;
+#pragma unroll 1
+            for (int g = 0; g < BPT; g += 4) {
+                const uint4 n = *(const uint4*)&sm.hist[tid * BPT + g];
+                if ((n.x | n.y | n.z | n.w) == 0) continue;
+                uint32_t c;
+                uint64_t w;
+                bin_sums(tid * BPT + g, n.x, c, w);
+                c_sum += c, w_sum += w;
+                bin_sums(tid * BPT + g + 1, n.y, c, w);
+                c_sum += c, w_sum += w;
+                bin_sums(tid * BPT + g + 2, n.z, c, w);
+                c_sum += c, w_sum += w;
+                bin_sums(tid * BPT + g + 3, n.w, c, w);
+                c_sum += c, w_sum += w;
+            }
+            wave_scan(c_sum, w_sum);
+            sm.pc[tid] = c_sum;
+            sm.pw[tid] = w_sum;
+            if (lane == 63) {
+                sm.tc[wv] = c_sum;
+                sm.tw[wv] = w_sum;
+            }
+            __syncthreads();
+            if (wv == 0) {
+                uint32_t ic = lane < NW ? sm.tc[lane & (NW - 1)] : 0;
+                uint64_t iw = lane < NW ? sm.tw[lane & (NW - 1)] : 0;
+                wave_scan(ic, iw);
+                const uint32_t all_c = base_c + of_lane(ic, NW - 1);
+                const uint64_t all_w = base_w + of_lane(iw, NW - 1);
+                int again = 0, ask = 0;
+                if (main && step == 0 && !have) {
+                    main_c = all_c;
+                    kept_c = all_c + (uint32_t)max(below, 0);
+                    kept_w = all_w;
+                }
+                for (;;) {
+                    if (!have) {                       // the main window is the one that stands
+                        if (step == 0) {
+                            const bool further = kn < -win.max && kmin < -win.max;      // numbers below the window
+                            if (k > 0 && (uint32_t)k < kept_c) {
+                                count = have = true;
+                                bound = (uint32_t)k;
+                            } else if (further && below < 0 && (k > 0 || (a.kept && p >= 1.f))) {
+                                ask = 1;
+                                break;
+                            }
+                            step = 1;
+                            if (have && kept_c > main_c && (uint32_t)k > main_c) {      // it is below the window
+                                base_c = main_c;
+                                base_w = all_w;
+                                main = false;
+                                again = 1;
+                                win.hi = -win.max - 1;
+                                win.max = min(win.max + MAGS, KMAX);
+                                break;
+                            }
+                        }
+                        if (!have && step == 1) {
+                            step = 2;
+                            if (p < 1.f) {
+                                bound = same((uint64_t)ceil((double)p * (double)kept_w));
+                                bound = bound > 0 ? bound : 1;
+                                count = false;
+                                have = true;
+                            }
+                        }
+                        if (!have) {
+                            if (!DRAW) break;
+                            step = 3;
+                            const uint32_t word = a.noise ? a.noise[i] : counter_word(a.seed, STREAM_TOKEN, a.step, a.row0 + (uint32_t)i, 0);
+                            bound = same((uint64_t)(((double)word + 0.5) * 0x1p-32 * (double)kept_w) + 1);
+                            count = false;
+                            have = true;
+                        }
+                    }
+                    if (count && bound > all_c) {      // further down
+                        base_c = all_c;
+                        base_w = all_w;
+                        again = 1;
+                        win.hi = -win.max - 1;
+                        win.max = min(win.max + MAGS, KMAX);
+                        break;
+                    }
+                    // the wavefront, thread and bin where the running count or weight reaches the bound
+                    auto reached = [&](uint32_t c, uint64_t w) { return count ? c >= bound : w >= bound; };
+                    const int x = __builtin_ctzll(__ballot(reached(base_c + ic, base_w + iw)));
+                    uint32_t before_c = base_c + (x ? of_lane(ic, x - 1) : 0);
+                    uint64_t before_w = base_w + (x ? of_lane(iw, x - 1) : 0);
+                    const uint32_t lc = sm.pc[x * 64 + lane];
+                    const uint64_t lw = sm.pw[x * 64 + lane];
+                    const int y = __builtin_ctzll(__ballot(reached(before_c + lc, before_w + lw)));
+                    before_c += y ? of_lane(lc, y - 1) : 0;
+                    before_w += y ? of_lane(lw, y - 1) : 0;
+                    const int bin0 = (x * 64 + y) * BPT;
+                    uint32_t bc, sc;
+                    uint64_t bw, sw;
+                    bin_sums(bin0 + (lane & (BPT - 1)), sm.hist[bin0 + (lane & (BPT - 1))], bc, bw);
+                    sc = bc, sw = bw;
+                    scan_step<0x111, 0xF>(sc, sw);     // (BPT neighbours; those of other lanes are not looked at)
+                    scan_step<0x112, 0xF>(sc, sw);
+                    if constexpr (BPT > 4) {
+                        scan_step<0x114, 0xF>(sc, sw);
+                        scan_step<0x118, 0xF>(sc, sw);
+                    }
+                    const int z = __builtin_ctzll(__ballot(reached(before_c + sc, before_w + sw)));
+                    before_c += z ? of_lane(sc, z - 1) : 0;
+                    before_w += z ? of_lane(sw, z - 1) : 0;
+                    const uint32_t in_c = of_lane(bc, z);
+                    if (bin0 + z == ZERO && win.min() > 1) {       // among the numbers nearer to 0
+                        base_c = before_c;
+                        base_w = before_w;
+                        main = false;
+                        again = 1;
+                        win.lo = max(win.lo, 1 - win.min());
+                        win.hi = min(win.hi, win.min() - 1);
+                        win.max = max(win.min() - 1, MAGS);
+                        break;
+                    }
+                    last = win.key(bin0 + z);
+                    uint64_t one = 0;
+                    if (count) {
+                        j = (uint32_t)(bound - before_c);
+                        one = q.weigh ? same(weight(q, sm.tab, key_float(last))) : 0;
+                    } else {                           // the first j of them whose weights reach the bound
+                        const uint64_t lack = bound - before_w;
+                        one = same(weight(q, sm.tab, key_float(last)));
+                        j = same((uint32_t)((double)lack / (double)one));
+                        while (j * one < lack) ++j;
+                        while (j > 1 && (j - 1) * one >= lack) --j;
+                    }
+                    pick = j < in_c || step == 3;
+                    if (step == 3) break;
+                    kept_c = before_c + j;
+                    kept_w = before_w + j * one;
+                    have = false;
+                    if (!DRAW && (step == 2 || p >= 1.f)) break;
+                    if (!main) {
+                        main = true;
+                        again = 1;
+                        win = {mags, kmin, KMAX};
+                        base_c = 0;
+                        base_w = 0;
+                        break;
+                    }
+                }
+                if (lane == 0) {
+                    sm.again = again;
+                    sm.ask = ask;
+                    sm.next = win;
+                    sm.last = last;
+                    sm.pick = pick;
+                    sm.j = j;
+                }
+            }
+            __syncthreads();
+            if (same(sm.ask)) {
+                // numbers below the window
+                uint32_t x = 0;
+#pragma unroll
+                for (int y = 0; y < CH * 4; ++y)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x += key[y][e] >= kmin && key[y][e] < -win.max;
+                if (x) atomicAdd(&sm.below, x);
+                __syncthreads();
+                below = same((int)sm.below);
+            } else if (!same(sm.again)) {
+                break;
+            }
+            win.max = same(sm.next.max);
+            win.lo = same(sm.next.lo);
+            win.hi = same(sm.next.hi);
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < BPT / 4; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
+            if (tid == 0) {
+                sm.zero_c = 0;
+                sm.zero_w = 0;
+            }
+            __syncthreads();
+        }
+        last = same(sm.last);
+        pick = same(sm.pick);
+        j = same(sm.j);
+    }
+    // the j-th number equal to `last`, in the order of classes
+    int last_v = INT_MAX;
+    if (pick) {
+        const u16x2 is = (u16x2)(unsigned short)(short)last;
+        auto bits = [&](int c) {     // of this thread's 8 classes
+            uint32_t x = 0;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                x |= (uint32_t)((int)key[4 * c + y][0] == last) << (2 * y);
+                x |= (uint32_t)((int)key[4 * c + y][1] == last) << (2 * y + 1);
+            }
+            return x;
+        };
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            u16x2 d = __builtin_bit_cast(u16x2, key[4 * c]) ^ is;
+#pragma unroll
+            for (int y = 1; y < 4; ++y) d = __builtin_elementwise_min(d, __builtin_bit_cast(u16x2, key[4 * c + y]) ^ is);
+            uint32_t x = 0;
+            if (__ballot(d[0] == 0 || d[1] == 0)) x = wave_scan((uint32_t)__popc(bits(c)));
+            if (lane == 63) sm.cell[c * NW + wv] = x;
+        }
+        __syncthreads();
+        // the cell of the j-th: each lane sums PER neighbours
+        constexpr int PER = (CH * NW + 63) / 64;
+        uint32_t cells[PER], sum = 0;
+#pragma unroll
+        for (int x = 0; x < PER; ++x) {
+            cells[x] = lane * PER + x < CH * NW ? sm.cell[lane * PER + x] : 0;
+            sum += cells[x];
+        }
+        const uint32_t inc = wave_scan(sum);
+        const int owner = __builtin_ctzll(__ballot(inc >= j));     // (j is at most their number)
+        uint32_t before = of_lane(inc - sum, owner);
+        int at = owner * PER;
+#pragma unroll
+        for (int x = 0; x < PER - 1; ++x) {
+            const uint32_t y = of_lane(cells[x], owner);
+            if (at == owner * PER + x && before + y < j) {
+                before += y;
+                ++at;
+            }
+        }
+        if (at % NW == wv) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (c == at / NW) {
+                    const uint32_t x = bits(c), mine = __popc(x), up = wave_scan(mine), want = j - before;
+                    if (up - mine < want && want <= up) {
+                        uint32_t y = x;
+                        for (uint32_t f = want - (up - mine); f > 1; --f) y &= y - 1;
+                        sm.at = (c * NT + tid) * 8 + __builtin_ctz(y);
+                    }
+                }
+        }
+        __syncthreads();
+        last_v = same(sm.at);
+    }
+    if (tid == 0) {
+        if (a.kept) a.kept[i] = (int32_t)kept_c;
+        if (DRAW) {
+            a.z[i] = last_v;
+            if (a.logp) {
+                const bool first = t == 0.f || k == 1;
+                a.logp[i] = first ? 0.f : (float)(((double)key_float(last) - (double)top) / (double)t - log(ldexp((double)kept_w, -a.frac)));
+            }
+        }
+    }
+    if constexpr (!DRAW) {
+        bf16_t* out = (bf16_t*)a.out + (int64_t)r * a.ld;
+        constexpr float largest = 0x1.FEp127f;     // (quotients do not become infinite)
+        const bool divide = t != 1.f && t != 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int v = (c * NT + tid) * 8;
+            if (v >= a.V) continue;
+            uint4 o = Elem<bf16_t>::NEG_INF4;
+            s16x2 x = key[4 * c];
+#pragma unroll
+            for (int y = 1; y < 4; ++y) x = __builtin_elementwise_max(x, key[4 * c + y]);
+            if (max((int)x[0], (int)x[1]) >= last) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int g = key[4 * c + e / 2][e & 1];
+                    float l = key_float(g);
+                    if (divide) l = fminf(fmaxf(l / t, -largest), largest);
+                    f[e] = g > last || (g == last && v + e <= last_v) ? l : -INFINITY;
+                }
+                o = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+            }
+            if (v + 8 <= a.V) {
+                *(uint4*)(out + v) = o;
+            } else {
+                const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (v + e < a.V) out[v + e] = (bf16_t)(w[e / 2] >> (16 * (e & 1)));
+            }
+        }
+    }
+}
+
 }  // namespace
+
+template <bool DRAW>
+static void launch_sample_keys(const SampleArgs& a, hipStream_t s) {
+    auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)a.n), dim3(threads), 0, s, a); };
+    if (a.V <= 2048) go(sample_keys_kernel<256, 1, DRAW>, 256);
+    else if (a.V <= 8192) go(sample_keys_kernel<256, 4, DRAW>, 256);
+    else if (a.V <= 16384) go(sample_keys_kernel<1024, 2, DRAW>, 1024);
+    else if (a.V <= 32768) go(sample_keys_kernel<1024, 4, DRAW>, 1024);
+    else if (a.V <= 57344) go(sample_keys_kernel<1024, 7, DRAW>, 1024);
+    else if (a.V <= 65536) go(sample_keys_kernel<1024, 8, DRAW>, 1024);
+    else go(sample_keys_kernel<1024, 16, DRAW>, 1024);
+}
 
 template <typename T, bool DRAW>
 static void launch_sample_t(const SampleArgs& a, hipStream_t s) {
+    if constexpr (sizeof(T) == 2) {
+        if (a.V <= 131072 && grid_fits(a.n, 1024)) return launch_sample_keys<DRAW>(a, s);
+    }
     const dim3 grid((unsigned)std::min<int64_t>(a.n, 2 * num_cus()));
     launch_k((sample_kernel<T, 1024, 0, DRAW>), grid, dim3(1024), 0, s, a);
 }
