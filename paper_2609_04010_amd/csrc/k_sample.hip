@@ -36,6 +36,7 @@ DD_DEV uint64_t place(float l, int v) { return ((uint64_t)value_key(l) << 32) | 
 
 constexpr int TAB = 64;      // 2^(-j / TAB)
 constexpr int LIST = 64;     // classes of a bin that are ordered one by one
+constexpr int EQUALS = 256;  // equal numbers that are
 
 template <int NT>
 struct SampleLds {
@@ -90,6 +91,17 @@ DD_DEV uint64_t weight(const RowScale& s, const double* tab, float l) {
     e = fma(x, e, 1.0);
     e = ldexp(e * tab[k & (TAB - 1)], s.frac - (k / TAB));
     return (uint64_t)__double_as_longlong(e + 0x1p52) - 0x4330000000000000ull;
+}
+
+// l / t, rounded to nearest, from y = 1 / t rounded to nearest: a quotient within two steps, then twice corrected by what
+// it leaves.  For |l| in [2^-100, 2^90] and t in [2^-30, 2^30] (below, within a step).
+DD_DEV float quotient(float l, float t, float y) {
+    float q = l * y;
+    q = fmaf(fmaf(-q, t, l), y, q);
+    return fmaf(fmaf(-q, t, l), y, q);
+}
+DD_DEV bool quotient_fits(float t, float a, float b) {
+    return t >= 0x1p-30f && t <= 0x1p30f && fabsf(a) < 0x1p90f && fabsf(b) < 0x1p90f;
 }
 
 DD_DEV int bin_of(const RowScale& s, float l, int last) { return (int)fminf((s.top - l) * s.per, (float)last); }
@@ -455,7 +467,6 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
-constexpr int MAGS = 2047, ZERO = MAGS, KBINS = 2 * MAGS + 2;    // bins: positive, near 0, negative, one to spare
 constexpr int KMAX = 0x7F7F, KINF = 0x7F80;                      // keys of the largest number and of infinity
 
 DD_DEV s16x2 keys_of(uint32_t w) {
@@ -498,8 +509,11 @@ DD_DEV uint32_t wave_scan(uint32_t c) {
     return c;
 }
 
-// The window that is counted: largest magnitude (the smallest is w_max - MAGS + 1), and the keys that count.
+// The window that is counted: MAGS magnitudes up to `max`, of either sign, and the keys that count.  Bins: positive, near 0,
+// negative, one to spare.
+template <int MAGS>
 struct Window {
+    static constexpr int ZERO = MAGS, BINS = 2 * MAGS + 2;
     int max, lo, hi;
     DD_DEV int min() const { return max - MAGS + 1; }
     DD_DEV int key(int bin) const { return bin < ZERO ? max - bin : bin == ZERO ? 0 : -(bin - ZERO - 1 + min()); }
@@ -508,24 +522,30 @@ struct Window {
 template <int NT, int CH>
 struct KeyLds {
     static constexpr int NW = NT / 64;
+    using Win = Window<NT < 512 ? 2047 : 4095>;      // (a wider one is cleared and summed longer: not for short rows)
     double tab[TAB];
-    uint32_t hist[KBINS + 64];       // counts; numbers outside the window go behind them, lane by lane
-    uint64_t pw[NT], tw[NW];         // weights of a thread's bins and those before them in its wavefront; of a wavefront's
-    uint32_t pc[NT], tc[NW];         // counts, likewise
-    int hi[NW], lo[NW];
+    uint32_t hist[Win::BINS + 64];       // counts; numbers outside the window go behind them, lane by lane
+    // bins in groups of 256: weights of four neighbours and those before them in their group; of a group.  Counts likewise
+    static constexpr int GROUPS = Win::BINS / 256;
+    uint64_t pw[Win::BINS / 4], tw[GROUPS];
+    uint32_t pc[Win::BINS / 4], tc[GROUPS];
+    int hi[NW], lo[NW], kth[NW];
     uint64_t zero_w;
     uint32_t zero_c, below;
+    __attribute__((aligned(16))) int list[EQUALS];
+    int listed;                      // classes of equal numbers, where they are few
     uint32_t cell[CH * NW];          // equal numbers per chunk and wavefront
     // what wavefront 0 decided: count this window (or, `ask`, the numbers below it), or the j-th of the numbers of key `last`
-    Window next;
+    Win next;
     int again, ask, last, pick, at;
-    uint32_t j;
+    uint32_t j, n;
 };
 
 template <int NT, int CH, bool DRAW>
-__global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys_kernel(SampleArgs a) {
+__global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
     using L = KeyLds<NT, CH>;
-    constexpr int NW = L::NW, BPT = KBINS / NT;
+    using Win = typename L::Win;
+    constexpr int NW = L::NW, MAGS = Win::ZERO, ZERO = Win::ZERO, KBINS = Win::BINS, GROUPS = L::GROUPS;
     __shared__ __attribute__((aligned(16))) L sm;
     const int tid = threadIdx.x, lane = tid & 63, wv = same(tid >> 6);
     const int i = blockIdx.x;
@@ -548,8 +568,10 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
             if (v < a.V) u[c] = *(const uint4*)(row + v);
         }
         if (tid < TAB) sm.tab[tid] = power_table.v[tid];
+        static_assert(NT >= EQUALS, "a thread for each");
+        if (tid < EQUALS) sm.list[tid] = INT_MAX;
 #pragma unroll
-        for (int b = 0; b < BPT / 4; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
+        for (int b = 0; b < KBINS / 4 / NT; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int v = (c * NT + tid) * 8;
@@ -564,7 +586,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
     const float t = a.temperature ? a.temperature[set] : 1.f, p = a.top_p ? a.top_p[set] : 1.f, m = a.min_p ? a.min_p[set] : 0.f;
     const int k = a.top_k ? a.top_k[set] : 0;
     // largest and smallest key (NaN stands beyond the infinities)
-    int kx, kn;
+    int kx, kn, kmin = -KMAX;    // kmin: the smallest that counts
     {
         s16x2 x = key[0], n = key[0];
 #pragma unroll
@@ -574,6 +596,19 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
         }
         kx = max((int)x[0], (int)x[1]);
         kn = min((int)n[0], (int)n[1]);
+        // top-k: the ceil(k / NW)-th largest of a wavefront's lanes' largest numbers; as many numbers reach the smallest of
+        // those of all wavefronts as k at least, and what is smaller need not be counted
+        int kth = -KINF;
+        if (k > 1 && k <= NT) {
+            const int rank = (k + NW - 1) / NW;
+            int lo = -KINF - 1, hi = KINF + 255;       // (above lo: rank lanes or more; above hi: fewer)
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (__popcll(__ballot(kx > mid)) >= rank) lo = mid;
+                else hi = mid;
+            }
+            kth = hi;
+        }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             kx = max(kx, __shfl_xor(kx, o, 64));
@@ -582,21 +617,26 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
         if (lane == 0) {
             sm.hi[wv] = kx;
             sm.lo[wv] = kn;
+            sm.kth[wv] = kth;
         }
         if (tid == 0) {
+            sm.listed = 0;
             sm.zero_c = sm.below = 0;
             sm.zero_w = 0;
         }
         __syncthreads();
         kx = sm.hi[lane & (NW - 1)];
         kn = sm.lo[lane & (NW - 1)];
+        kth = sm.kth[lane & (NW - 1)];
 #pragma unroll
         for (int o = NW / 2; o > 0; o >>= 1) {
             kx = max(kx, __shfl_xor(kx, o, 64));
             kn = min(kn, __shfl_xor(kn, o, 64));
+            kth = min(kth, __shfl_xor(kth, o, 64));
         }
         kx = same(kx);
         kn = same(kn);
+        kmin = max(kmin, same(kth));
     }
     const bool settings = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f;   // (false for NaN)
     if (kx >= KINF || kx <= -KINF || kn < -KINF || !settings) {
@@ -616,7 +656,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
     }
     const float top = key_float(kx);
     const RowScale q = {top, 0.f, 0.f, TAB * 1.4426950408889634 / (double)t, a.frac, DRAW || p < 1.f};
-    int kmin = -KMAX;            // the smallest key that min-p leaves
+    const bool few = kmin > -KMAX;       // (top-k has said so: most numbers do not count)
     int mags;                    // the largest magnitude that can matter
     {
         float b = top - 34.f * t;
@@ -627,21 +667,31 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                 float f = (float)e;
                 if ((double)f < e) f = key_value(value_key(f) - 1);    // the next number above
                 const uint32_t u = __float_as_uint(f);
-                kmin = same((int32_t)u < 0 ? -(int)((u & 0x7FFFFFFFu) >> 16) : (int)((u + 0xFFFFu) >> 16));
-                b = fmaxf(b, f);
+                kmin = max(kmin, same((int32_t)u < 0 ? -(int)((u & 0x7FFFFFFFu) >> 16) : (int)((u + 0xFFFFu) >> 16)));
             }
         }
+        b = fmaxf(b, key_float(kmin));
         mags = min(KMAX, (int)((__float_as_uint(b) & 0x7FFFFFFFu) >> 16) + 1);
         mags = same(max(max(mags, kx < 0 ? -kx : kx), MAGS));
     }
     int last = kmin, pick = 0;           // key of the last that stays (or of the draw); whether the j-th of them is looked for
-    uint32_t j = 1, kept_c = 1;
+    uint32_t j = 1, n = INT_MAX, kept_c = 1;     // n: how many there are (or more)
     uint64_t kept_w = 0;
     if (t == 0.f || k == 1) {
         last = kx;
         pick = 1;
-    } else if (q.weigh || k > 0 || a.kept) {
-        Window win = {mags, kmin, KMAX};
+    } else if (!q.weigh && k <= 0) {
+        if (a.kept) {                    // what min-p leaves
+            uint32_t x = 0;
+#pragma unroll
+            for (int y = 0; y < CH * 4; ++y) x += (uint32_t)((int)key[y][0] >= kmin) + (uint32_t)((int)key[y][1] >= kmin);
+            x = wave_scan(x);
+            if (lane == 63) atomicAdd(&sm.below, x);
+            __syncthreads();
+            kept_c = sm.below;
+        }
+    } else {
+        Win win = {mags, kmin, KMAX};
         // of wavefront 0: sums before the window; top-k, top-p and draw done; what is looked for
         uint32_t base_c = 0, main_c = 0;
         uint64_t base_w = 0, bound = 0;
@@ -657,6 +707,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                 const u16x2 sh = (u16x2)(unsigned short)(win.max + win.min() - (MAGS + 1)), out = (u16x2)(unsigned short)(KBINS + lane);
 #pragma unroll
                 for (int x = 0; x < CH * 4; ++x) {
+                    if (few && !__any(max((int)key[x][0], (int)key[x][1]) >= kmin)) continue;
                     const u16x2 d = hi - __builtin_bit_cast(u16x2, key[x]);
                     u16x2 b = __builtin_elementwise_min(d, __builtin_elementwise_max(mid, __builtin_elementwise_sub_sat(d, sh)));
                     b = __builtin_elementwise_min(b, out);
@@ -702,47 +753,56 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                 }
                 __syncthreads();
             }
-            // count and weight of a bin
-            auto bin_sums = [&](int bin, uint32_t n, uint32_t& c, uint64_t& w) {
+            // count and weight of a bin, and the weight of one of its numbers
+            auto bin_sums = [&](int bin, uint32_t n, uint32_t& c, uint64_t& w) -> uint64_t {
                 const int f = win.key(bin);
                 c = f < win.lo || f > win.hi || bin == KBINS - 1 ? 0 : n;
-                w = c && q.weigh ? c * weight(q, sm.tab, key_float(f)) : 0;
+                const uint64_t one = q.weigh ? weight(q, sm.tab, key_float(f)) : 0;
+                w = c * one;
                 if (near && bin == ZERO) {
                     c = sm.zero_c;
                     w = sm.zero_w;
                 }
+                return one;
             };
-            uint32_t c_sum = 0;
-            uint64_t w_sum = 0;
+            // (every wavefront a group of each part of the bins: most numbers stand in few of them)
 #pragma unroll 1
-            for (int g = 0; g < BPT; g += 4) {
-                const uint4 n = *(const uint4*)&sm.hist[tid * BPT + g];
-                if ((n.x | n.y | n.z | n.w) == 0) continue;
-                uint32_t c;
-                uint64_t w;
-                bin_sums(tid * BPT + g, n.x, c, w);
+            for (int g = wv; g < GROUPS; g += NW) {
+                const int b = (g * 64 + lane) * 4;
+                const uint4 n = *(const uint4*)&sm.hist[b];
+                if (!__any((n.x | n.y | n.z | n.w) != 0)) {
+                    if (lane == 0) {
+                        sm.tc[g] = 0;
+                        sm.tw[g] = 0;
+                    }
+                    continue;
+                }
+                uint32_t c, c_sum = 0;
+                uint64_t w, w_sum = 0;
+                bin_sums(b, n.x, c, w);
                 c_sum += c, w_sum += w;
-                bin_sums(tid * BPT + g + 1, n.y, c, w);
+                bin_sums(b + 1, n.y, c, w);
                 c_sum += c, w_sum += w;
-                bin_sums(tid * BPT + g + 2, n.z, c, w);
+                bin_sums(b + 2, n.z, c, w);
                 c_sum += c, w_sum += w;
-                bin_sums(tid * BPT + g + 3, n.w, c, w);
+                bin_sums(b + 3, n.w, c, w);
                 c_sum += c, w_sum += w;
-            }
-            wave_scan(c_sum, w_sum);
-            sm.pc[tid] = c_sum;
-            sm.pw[tid] = w_sum;
-            if (lane == 63) {
-                sm.tc[wv] = c_sum;
-                sm.tw[wv] = w_sum;
+                wave_scan(c_sum, w_sum);
+                sm.pc[g * 64 + lane] = c_sum;
+                sm.pw[g * 64 + lane] = w_sum;
+                if (lane == 63) {
+                    sm.tc[g] = c_sum;
+                    sm.tw[g] = w_sum;
+                }
             }
             __syncthreads();
             if (wv == 0) {
-                uint32_t ic = lane < NW ? sm.tc[lane & (NW - 1)] : 0;
-                uint64_t iw = lane < NW ? sm.tw[lane & (NW - 1)] : 0;
+                static_assert(GROUPS <= 64, "a group per lane");
+                uint32_t ic = lane < GROUPS ? sm.tc[lane & (GROUPS - 1)] : 0;
+                uint64_t iw = lane < GROUPS ? sm.tw[lane & (GROUPS - 1)] : 0;
                 wave_scan(ic, iw);
-                const uint32_t all_c = base_c + of_lane(ic, NW - 1);
-                const uint64_t all_w = base_w + of_lane(iw, NW - 1);
+                const uint32_t all_c = base_c + of_lane(ic, 63);
+                const uint64_t all_w = base_w + of_lane(iw, 63);
                 int again = 0, ask = 0;
                 if (main && step == 0 && !have) {
                     main_c = all_c;
@@ -797,7 +857,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                         win.max = min(win.max + MAGS, KMAX);
                         break;
                     }
-                    // the wavefront, thread and bin where the running count or weight reaches the bound
+                    // the group, four neighbours and bin where the running count or weight reaches the bound
                     auto reached = [&](uint32_t c, uint64_t w) { return count ? c >= bound : w >= bound; };
                     const int x = __builtin_ctzll(__ballot(reached(base_c + ic, base_w + iw)));
                     uint32_t before_c = base_c + (x ? of_lane(ic, x - 1) : 0);
@@ -807,17 +867,13 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                     const int y = __builtin_ctzll(__ballot(reached(before_c + lc, before_w + lw)));
                     before_c += y ? of_lane(lc, y - 1) : 0;
                     before_w += y ? of_lane(lw, y - 1) : 0;
-                    const int bin0 = (x * 64 + y) * BPT;
+                    const int bin0 = (x * 64 + y) * 4;
                     uint32_t bc, sc;
                     uint64_t bw, sw;
-                    bin_sums(bin0 + (lane & (BPT - 1)), sm.hist[bin0 + (lane & (BPT - 1))], bc, bw);
+                    const uint64_t b1 = bin_sums(bin0 + (lane & 3), sm.hist[bin0 + (lane & 3)], bc, bw);
                     sc = bc, sw = bw;
-                    scan_step<0x111, 0xF>(sc, sw);     // (BPT neighbours; those of other lanes are not looked at)
+                    scan_step<0x111, 0xF>(sc, sw);     // (of lanes 0 to 3; the others are not looked at)
                     scan_step<0x112, 0xF>(sc, sw);
-                    if constexpr (BPT > 4) {
-                        scan_step<0x114, 0xF>(sc, sw);
-                        scan_step<0x118, 0xF>(sc, sw);
-                    }
                     const int z = __builtin_ctzll(__ballot(reached(before_c + sc, before_w + sw)));
                     before_c += z ? of_lane(sc, z - 1) : 0;
                     before_w += z ? of_lane(sw, z - 1) : 0;
@@ -833,18 +889,17 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                         break;
                     }
                     last = win.key(bin0 + z);
-                    uint64_t one = 0;
+                    const uint64_t one = of_lane(b1, z);
                     if (count) {
                         j = (uint32_t)(bound - before_c);
-                        one = q.weigh ? same(weight(q, sm.tab, key_float(last))) : 0;
                     } else {                           // the first j of them whose weights reach the bound
                         const uint64_t lack = bound - before_w;
-                        one = same(weight(q, sm.tab, key_float(last)));
                         j = same((uint32_t)((double)lack / (double)one));
                         while (j * one < lack) ++j;
                         while (j > 1 && (j - 1) * one >= lack) --j;
                     }
                     pick = j < in_c || step == 3;
+                    n = in_c;
                     if (step == 3) break;
                     kept_c = before_c + j;
                     kept_w = before_w + j * one;
@@ -866,6 +921,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
                     sm.last = last;
                     sm.pick = pick;
                     sm.j = j;
+                    sm.n = n;
                 }
             }
             __syncthreads();
@@ -887,7 +943,7 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
             win.hi = same(sm.next.hi);
             __syncthreads();
 #pragma unroll
-            for (int b = 0; b < BPT / 4; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
+            for (int b = 0; b < KBINS / 4 / NT; ++b) ((uint4*)sm.hist)[b * NT + tid] = make_uint4(0u, 0u, 0u, 0u);
             if (tid == 0) {
                 sm.zero_c = 0;
                 sm.zero_w = 0;
@@ -897,61 +953,85 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
         last = same(sm.last);
         pick = same(sm.pick);
         j = same(sm.j);
+        n = same(sm.n);
     }
     // the j-th number equal to `last`, in the order of classes
     int last_v = INT_MAX;
     if (pick) {
         const u16x2 is = (u16x2)(unsigned short)(short)last;
-        auto bits = [&](int c) {     // of this thread's 8 classes
-            uint32_t x = 0;
+        if (n <= EQUALS) {           // all of them, and those before each counted
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                x |= (uint32_t)((int)key[4 * c + y][0] == last) << (2 * y);
-                x |= (uint32_t)((int)key[4 * c + y][1] == last) << (2 * y + 1);
+            for (int c = 0; c < CH; ++c) {
+                u16x2 d = __builtin_bit_cast(u16x2, key[4 * c]) ^ is;
+#pragma unroll
+                for (int y = 1; y < 4; ++y) d = __builtin_elementwise_min(d, __builtin_bit_cast(u16x2, key[4 * c + y]) ^ is);
+                if (d[0] != 0 && d[1] != 0) continue;
+                uint32_t x = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x |= (uint32_t)((int)key[4 * c + e / 2][e & 1] == last) << e;
+                int to = atomicAdd(&sm.listed, __popc(x));
+                for (; x; x &= x - 1) sm.list[to++] = (c * NT + tid) * 8 + __builtin_ctz(x);
             }
-            return x;
-        };
+            __syncthreads();
+            if (tid < (int)n) {
+                const int v = sm.list[tid];
+                uint32_t before = 0;
+                for (int x = 0; x < (int)n; x += 16) {       // (behind them stands INT_MAX)
+                    int4 y[4];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            u16x2 d = __builtin_bit_cast(u16x2, key[4 * c]) ^ is;
+                    for (int z = 0; z < 4; ++z) y[z] = *(const int4*)&sm.list[x + 4 * z];
 #pragma unroll
-            for (int y = 1; y < 4; ++y) d = __builtin_elementwise_min(d, __builtin_bit_cast(u16x2, key[4 * c + y]) ^ is);
-            uint32_t x = 0;
-            if (__ballot(d[0] == 0 || d[1] == 0)) x = wave_scan((uint32_t)__popc(bits(c)));
-            if (lane == 63) sm.cell[c * NW + wv] = x;
-        }
-        __syncthreads();
-        // the cell of the j-th: each lane sums PER neighbours
-        constexpr int PER = (CH * NW + 63) / 64;
-        uint32_t cells[PER], sum = 0;
-#pragma unroll
-        for (int x = 0; x < PER; ++x) {
-            cells[x] = lane * PER + x < CH * NW ? sm.cell[lane * PER + x] : 0;
-            sum += cells[x];
-        }
-        const uint32_t inc = wave_scan(sum);
-        const int owner = __builtin_ctzll(__ballot(inc >= j));     // (j is at most their number)
-        uint32_t before = of_lane(inc - sum, owner);
-        int at = owner * PER;
-#pragma unroll
-        for (int x = 0; x < PER - 1; ++x) {
-            const uint32_t y = of_lane(cells[x], owner);
-            if (at == owner * PER + x && before + y < j) {
-                before += y;
-                ++at;
-            }
-        }
-        if (at % NW == wv) {
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-                if (c == at / NW) {
-                    const uint32_t x = bits(c), mine = __popc(x), up = wave_scan(mine), want = j - before;
-                    if (up - mine < want && want <= up) {
-                        uint32_t y = x;
-                        for (uint32_t f = want - (up - mine); f > 1; --f) y &= y - 1;
-                        sm.at = (c * NT + tid) * 8 + __builtin_ctz(y);
-                    }
+                    for (int z = 0; z < 4; ++z) before += (y[z].x < v) + (y[z].y < v) + (y[z].z < v) + (y[z].w < v);
                 }
+                if (before == j - 1) sm.at = v;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                u16x2 d = (u16x2)(unsigned short)0;        // how many are not equal
+#pragma unroll
+                for (int y = 0; y < 4; ++y) d += __builtin_elementwise_min(__builtin_bit_cast(u16x2, key[4 * c + y]) ^ is, (u16x2)(unsigned short)1);
+                uint32_t x = 8 - d[0] - d[1];
+                if (__ballot(x != 0)) x = wave_scan(x);
+                if (lane == 63) sm.cell[c * NW + wv] = x;
+            }
+            __syncthreads();
+            // the cell of the j-th: each lane sums PER neighbours
+            constexpr int PER = (CH * NW + 63) / 64;
+            uint32_t cells[PER], sum = 0;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                cells[x] = lane * PER + x < CH * NW ? sm.cell[lane * PER + x] : 0;
+                sum += cells[x];
+            }
+            const uint32_t inc = wave_scan(sum);
+            const int owner = __builtin_ctzll(__ballot(inc >= j));     // (j is at most their number)
+            uint32_t before = of_lane(inc - sum, owner);
+            int at = owner * PER;
+#pragma unroll
+            for (int x = 0; x < PER - 1; ++x) {
+                const uint32_t y = of_lane(cells[x], owner);
+                if (at == owner * PER + x && before + y < j) {
+                    before += y;
+                    ++at;
+                }
+            }
+            if (at % NW == wv) {
+                // (from memory again: registers have no numbers)
+                const int v = (at / NW * NT + tid) * 8;
+                const uint4 u = v < a.V ? *(const uint4*)(row + v) : Elem<bf16_t>::NEG_INF4;
+                uint32_t x = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
+                    x |= (uint32_t)(v + e < a.V && (int)keys_of(w)[e & 1] == last) << e;
+                }
+                const uint32_t mine = __popc(x), up = wave_scan(mine), want = j - before;
+                if (up - mine < want && want <= up) {
+                    for (uint32_t f = want - (up - mine); f > 1; --f) x &= x - 1;
+                    sm.at = v + __builtin_ctz(x);
+                }
+            }
         }
         __syncthreads();
         last_v = same(sm.at);
@@ -969,22 +1049,28 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
     if constexpr (!DRAW) {
         bf16_t* out = (bf16_t*)a.out + (int64_t)r * a.ld;
         constexpr float largest = 0x1.FEp127f;     // (quotients do not become infinite)
-        const bool divide = t != 1.f && t != 0.f;
+        const bool divide = t != 1.f && t != 0.f, fast = quotient_fits(t, top, key_float(last));
+        const float rt = 1.f / t;
+        uint32_t some = 0;                         // chunks in which something stays
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            s16x2 x = key[4 * c];
+#pragma unroll
+            for (int y = 1; y < 4; ++y) x = __builtin_elementwise_max(x, key[4 * c + y]);
+            some |= (uint32_t)(max((int)x[0], (int)x[1]) >= last) << c;
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int v = (c * NT + tid) * 8;
             if (v >= a.V) continue;
             uint4 o = Elem<bf16_t>::NEG_INF4;
-            s16x2 x = key[4 * c];
-#pragma unroll
-            for (int y = 1; y < 4; ++y) x = __builtin_elementwise_max(x, key[4 * c + y]);
-            if (max((int)x[0], (int)x[1]) >= last) {
+            if (some >> c & 1) {
                 float f[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int g = key[4 * c + e / 2][e & 1];
                     float l = key_float(g);
-                    if (divide) l = fminf(fmaxf(l / t, -largest), largest);
+                    if (divide) l = fast ? quotient(l, t, rt) : fminf(fmaxf(l / t, -largest), largest);
                     f[e] = g > last || (g == last && v + e <= last_v) ? l : -INFINITY;
                 }
                 o = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
@@ -1006,12 +1092,16 @@ __global__ __launch_bounds__(NT, NT == 1024 && CH <= 8 ? 8 : 4) void sample_keys
 template <bool DRAW>
 static void launch_sample_keys(const SampleArgs& a, hipStream_t s) {
     auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)a.n), dim3(threads), 0, s, a); };
+    // A row's time is that of its phases one behind the other: with a CU for each row it ends sooner in 1024 threads; where
+    // rows wait for CUs, two of 512 threads on a CU do less work each.
+    const bool few = a.n <= num_cus();
     if (a.V <= 2048) go(sample_keys_kernel<256, 1, DRAW>, 256);
     else if (a.V <= 8192) go(sample_keys_kernel<256, 4, DRAW>, 256);
-    else if (a.V <= 16384) go(sample_keys_kernel<1024, 2, DRAW>, 1024);
-    else if (a.V <= 32768) go(sample_keys_kernel<1024, 4, DRAW>, 1024);
-    else if (a.V <= 57344) go(sample_keys_kernel<1024, 7, DRAW>, 1024);
-    else if (a.V <= 65536) go(sample_keys_kernel<1024, 8, DRAW>, 1024);
+    else if (a.V <= 16384) go(sample_keys_kernel<512, 4, DRAW>, 512);
+    else if (a.V <= 32768) go(sample_keys_kernel<512, 8, DRAW>, 512);
+    else if (a.V <= 57344 && few) go(sample_keys_kernel<1024, 7, DRAW>, 1024);
+    else if (a.V <= 53248) go(sample_keys_kernel<512, 13, DRAW>, 512);
+    else if (a.V <= 65536) go(sample_keys_kernel<512, 16, DRAW>, 512);
     else go(sample_keys_kernel<1024, 16, DRAW>, 1024);
 }
 
