@@ -1104,7 +1104,7 @@ dd_status dd_token_sample(const void* logits, int32_t logits_dtype, int64_t ld, 
     DD_CHECK(z_out && (logits || rows == 0), DD_E_ARG, "NULL pointer argument");
     DD_CHECK(((uintptr_t)logits & 15) == 0, DD_E_ARG, "logits must be 16-byte aligned");
     SampleArgs a = {logits, ld, rows, V, row_ids, n, draws_per_seq, how->temperature, how->top_k, how->top_p, how->min_p,
-                    noise_words, seed, step, row0, z_out, logp, nullptr, n_kept, dev_err, 0};
+                    noise_words, seed, step, row0, z_out, logp, nullptr, n_kept, dev_err, 0, 1};
     return launch_sample(a, logits_dtype, true, (hipStream_t)stream);
 }
 
@@ -1116,7 +1116,7 @@ dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t l
     DD_CHECK(logits && out, DD_E_ARG, "NULL pointer argument");
     DD_CHECK((((uintptr_t)logits | (uintptr_t)out) & 15) == 0, DD_E_ARG, "logits and out must be 16-byte aligned");
     SampleArgs a = {logits, ld, rows, V, nullptr, rows, rows_per_seq, how->temperature, how->top_k, how->top_p, how->min_p,
-                    nullptr, 0, 0, 0, nullptr, nullptr, out, n_kept, dev_err, 0};
+                    nullptr, 0, 0, 0, nullptr, nullptr, out, n_kept, dev_err, 0, 1};
     return launch_sample(a, logits_dtype, false, (hipStream_t)stream);
 }
 

@@ -35,30 +35,11 @@ DD_DEV float key_value(uint32_t k) {
 DD_DEV uint64_t place(float l, int v) { return ((uint64_t)value_key(l) << 32) | (uint32_t)v; }
 
 constexpr int TAB = 64;      // 2^(-j / TAB)
-constexpr int LIST = 64;     // classes of a bin that are ordered one by one
 constexpr int EQUALS = 256;  // equal numbers that are
 
-template <int NT>
-struct SampleLds {
-    static constexpr int NB = 2 * NT, NW = NT / 64;
-    double tab[TAB];
-    uint64_t w1[NB], w2[NB];    // weights of the bins, then their inclusive prefix sums; of the row, of a bin that is cut again
-    uint32_t c1[NB], c2[NB];    // counts, likewise
-    uint64_t list[LIST];
-    uint64_t lo[NW], hi[NW];
-    float mx[NW], mn[NW];
-    uint64_t wsum[NW];
-    uint32_t csum[NW];
-    int bad[NW];
-    // what a search found
-    uint64_t base_w, in_w, at;
-    uint32_t base_c, in_c;
-    int bin, listed;
-};
-
-// what a row's weights and bins are made of
+// what a row's weights are made of
 struct RowScale {
-    float top, least, per;   // largest logit; smallest that min-p leaves; bins per unit of l
+    float top, least;        // largest logit; smallest that counts
     double turn;             // TAB log2(e) / temperature
     int frac;                // weights are multiples of 2^-frac
     bool weigh;              // sums of weights are needed
@@ -102,358 +83,6 @@ DD_DEV float quotient(float l, float t, float y) {
 }
 DD_DEV bool quotient_fits(float t, float a, float b) {
     return t >= 0x1p-30f && t <= 0x1p30f && fabsf(a) < 0x1p90f && fabsf(b) < 0x1p90f;
-}
-
-DD_DEV int bin_of(const RowScale& s, float l, int last) { return (int)fminf((s.top - l) * s.per, (float)last); }
-
-// inclusive prefix sums of c and w over the bins, in place
-template <int NT>
-DD_DEV void scan_bins(SampleLds<NT>& sm, uint32_t* c, uint64_t* w, bool weigh) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    uint32_t c0 = c[2 * tid], c1 = c0 + c[2 * tid + 1], cs = c1;
-    uint64_t w0 = weigh ? w[2 * tid] : 0, w1 = w0 + (weigh ? w[2 * tid + 1] : 0), ws = w1;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t cu = __shfl_up(cs, o, 64);
-        const uint64_t wu = __shfl_up(ws, o, 64);
-        if (lane >= o) {
-            cs += cu;
-            ws += wu;
-        }
-    }
-    if (lane == 63) {
-        sm.csum[wv] = cs;
-        sm.wsum[wv] = ws;
-    }
-    __syncthreads();
-    uint32_t cb = cs - c1;
-    uint64_t wb = ws - w1;
-    for (int i = 0; i < wv; ++i) {
-        cb += sm.csum[i];
-        wb += sm.wsum[i];
-    }
-    c[2 * tid] = cb + c0;
-    c[2 * tid + 1] = cb + c1;
-    w[2 * tid] = wb + w0;
-    w[2 * tid + 1] = wb + w1;
-    __syncthreads();
-}
-
-// the bin in which the running count (COUNT) or weight reaches t, t >= 1 and no more than all bins together hold
-template <int NT>
-DD_DEV void find_bin(SampleLds<NT>& sm, const uint32_t* c, const uint64_t* w, bool count, uint64_t t) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int b = 2 * threadIdx.x + k;
-        const uint32_t ce = b ? c[b - 1] : 0;
-        const uint64_t we = b ? w[b - 1] : 0;
-        if (count ? (ce < t && t <= c[b]) : (we < t && t <= w[b])) {
-            sm.bin = b;
-            sm.base_c = ce;
-            sm.base_w = we;
-            sm.in_c = c[b] - ce;
-        }
-    }
-    __syncthreads();
-}
-
-// T: logits; NT: threads; RES: 16-byte chunks of a row that a thread keeps in registers (0: read again for each pass);
-// DRAW: a token per draw (else: the row with what stays)
-template <typename T, int NT, int RES, bool DRAW>
-__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
-    using L = SampleLds<NT>;
-    constexpr int E = Elem<T>::E, NB = L::NB, NW = L::NW;
-    __shared__ L sm;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int chunks = RES > 0 ? RES : (a.V + NT * E - 1) / (NT * E);
-    if (tid < TAB) sm.tab[tid] = power_table.v[tid];
-    for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
-        int r = i;
-        if (DRAW && a.row_ids) {
-            r = a.row_ids[i];
-            if (r < 0 || r >= a.rows) {
-                if (r != -1 && tid == 0 && a.err) atomicOr(a.err, DD_DEVERR_SAMPLING);
-                continue;
-            }
-        }
-        const T* row = (const T*)a.logits + (int64_t)r * a.ld;
-        const int s = i / a.per;
-        const float t = a.temperature ? a.temperature[s] : 1.f, p = a.top_p ? a.top_p[s] : 1.f, m = a.min_p ? a.min_p[s] : 0.f;
-        const int k = a.top_k ? a.top_k[s] : 0;
-        auto chunk = [&](int c) -> uint4 {
-            const int v = (c * NT + tid) * E;
-            if (v >= a.V) return Elem<T>::NEG_INF4;
-            uint4 u = *(const uint4*)(row + v);
-            if (v + E > a.V) Elem<T>::clip(u, a.V - v);
-            return u;
-        };
-        uint4 reg[RES > 0 ? RES : 1];
-        if constexpr (RES > 0) {
-#pragma unroll
-            for (int c = 0; c < RES; ++c) reg[c] = chunk(c);
-        }
-        auto each = [&](auto&& f) {   // f(logit, class) for this thread's classes
-            if constexpr (RES > 0) {
-#pragma unroll
-                for (int c = 0; c < RES; ++c)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) f(Elem<T>::get(reg[c], e), (c * NT + tid) * E + e);
-            } else {
-                for (int c = 0; c < chunks; ++c) {
-                    const uint4 u = chunk(c);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) f(Elem<T>::get(u, e), (c * NT + tid) * E + e);
-                }
-            }
-        };
-
-        // largest and smallest finite logit, and whether there is anything that allows no choice
-        RowScale q;
-        {
-            float mx = -INFINITY, mn = INFINITY;
-            bool nan = false;
-            each([&](float l, int) {
-                mx = fmaxf(mx, l);
-                nan |= l != l;
-                if (l > -INFINITY) mn = fminf(mn, l);
-            });
-            for (int o = 32; o > 0; o >>= 1) {
-                mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-                mn = fminf(mn, __shfl_xor(mn, o, 64));
-            }
-            nan = __any(nan);
-            __syncthreads();   // the last row's results
-            if (lane == 0) {
-                sm.mx[wv] = mx;
-                sm.mn[wv] = mn;
-                sm.bad[wv] = nan;
-            }
-            for (int b = tid; b < NB; b += NT) {
-                sm.c1[b] = 0;
-                sm.w1[b] = 0;
-            }
-            __syncthreads();
-            for (int x = 0; x < NW; ++x) {
-                mx = fmaxf(mx, sm.mx[x]);
-                mn = fminf(mn, sm.mn[x]);
-                nan |= sm.bad[x] != 0;
-            }
-            const bool settings = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f;   // (false for NaN)
-            if (nan || mx == INFINITY || mx == -INFINITY || !settings) {
-                if (tid == 0) {
-                    if (a.err) atomicOr(a.err, settings ? DD_DEVERR_LOGITS : DD_DEVERR_SAMPLING);
-                    if (a.kept) a.kept[i] = 0;
-                    if (DRAW) {
-                        a.z[i] = 0;
-                        if (a.logp) a.logp[i] = NAN;
-                    }
-                }
-                if (!DRAW && a.out != a.logits) {
-                    T* out = (T*)a.out + (int64_t)r * a.ld;
-                    for (int v = tid; v < a.V; v += NT) out[v] = row[v];
-                }
-                continue;
-            }
-            q.top = mx;
-            const float reach = fminf(mx - mn, 32.f * t);
-            q.per = reach > 0.f ? fminf(NB / reach, 1e37f) : 0.f;
-            q.turn = TAB * 1.4426950408889634 / (double)t;
-            q.frac = a.frac;
-            q.least = -FLT_MAX;
-            if (m > 0.f && t > 0.f) {   // w >= m where l >= top + t log m
-                const double b = (double)mx + (double)t * log((double)m);
-                if (b > -FLT_MAX) {
-                    q.least = (float)b;
-                    if ((double)q.least < b) q.least = key_value(value_key(q.least) - 1);   // the next number above
-                }
-            }
-        }
-        uint64_t cut = ~0ull, kept_w = 0;   // the last place that stays, and the sums up to there
-        uint32_t kept_c = 0;
-        if (t == 0.f || k == 1) {
-            if (tid == 0) sm.bin = INT_MAX;
-            __syncthreads();
-            int v = INT_MAX;
-            each([&](float l, int c) { if (l == q.top) v = min(v, c); });
-            for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-            if (lane == 0) atomicMin(&sm.bin, v);
-            __syncthreads();
-            cut = place(q.top, sm.bin);
-            kept_c = 1;
-            if (DRAW) {
-                if (tid == 0) {
-                    a.z[i] = sm.bin;
-                    if (a.logp) a.logp[i] = 0.f;
-                    if (a.kept) a.kept[i] = 1;
-                }
-                continue;
-            }
-        } else if (DRAW || k > 0 || p < 1.f || a.kept) {
-            q.weigh = DRAW || p < 1.f;
-            each([&](float l, int) {
-                if (l >= q.least) {
-                    const int b = bin_of(q, l, NB - 1);
-                    atomicAdd(&sm.c1[b], 1u);
-                    if (q.weigh) atomicAdd((unsigned long long*)&sm.w1[b], (unsigned long long)weight(q, sm.tab, l));
-                }
-            });
-            __syncthreads();
-            scan_bins<NT>(sm, sm.c1, sm.w1, q.weigh);
-            kept_c = sm.c1[NB - 1];
-            kept_w = sm.w1[NB - 1];
-            // the first class at which the running count or weight reaches bound: its place in sm.at, the sums with it in
-            // sm.base_c and sm.base_w
-            auto search = [&](bool count, uint64_t bound) {
-                find_bin<NT>(sm, sm.c1, sm.w1, count, bound);
-                const int b1 = sm.bin;
-                uint32_t base_c = sm.base_c, n = sm.in_c;
-                uint64_t base_w = sm.base_w, lo = 0, hi = ~0ull;
-                auto mine = [&](float l, int v, uint64_t& c) {
-                    if (!(l >= q.least) || bin_of(q, l, NB - 1) != b1) return false;
-                    c = place(l, v);
-                    return c >= lo && c <= hi;
-                };
-                while (n > LIST) {
-                    uint64_t first = ~0ull, last = 0;
-                    each([&](float l, int v) {
-                        uint64_t c;
-                        if (mine(l, v, c)) {
-                            first = first < c ? first : c;
-                            last = last > c ? last : c;
-                        }
-                    });
-                    for (int o = 32; o > 0; o >>= 1) {
-                        const uint64_t f = __shfl_xor(first, o, 64), g = __shfl_xor(last, o, 64);
-                        first = first < f ? first : f;
-                        last = last > g ? last : g;
-                    }
-                    if (lane == 0) {
-                        sm.lo[wv] = first;
-                        sm.hi[wv] = last;
-                    }
-                    for (int b = tid; b < NB; b += NT) {
-                        sm.c2[b] = 0;
-                        sm.w2[b] = 0;
-                    }
-                    __syncthreads();
-                    for (int x = 0; x < NW; ++x) {
-                        first = first < sm.lo[x] ? first : sm.lo[x];
-                        last = last > sm.hi[x] ? last : sm.hi[x];
-                    }
-                    int shift = 0;
-                    while (((last - first) >> shift) >= NB) ++shift;
-                    each([&](float l, int v) {
-                        uint64_t c;
-                        if (mine(l, v, c)) {
-                            const int b = (int)((c - first) >> shift);
-                            atomicAdd(&sm.c2[b], 1u);
-                            if (q.weigh) atomicAdd((unsigned long long*)&sm.w2[b], (unsigned long long)weight(q, sm.tab, l));
-                        }
-                    });
-                    __syncthreads();
-                    scan_bins<NT>(sm, sm.c2, sm.w2, q.weigh);
-                    find_bin<NT>(sm, sm.c2, sm.w2, count, bound - (count ? (uint64_t)base_c : base_w));
-                    base_c += sm.base_c;
-                    base_w += sm.base_w;
-                    n = sm.in_c;
-                    lo = first + ((uint64_t)sm.bin << shift);
-                    hi = lo + ((1ull << shift) - 1);
-                    __syncthreads();
-                }
-                if (tid == 0) sm.listed = 0;
-                __syncthreads();
-                each([&](float l, int v) {
-                    uint64_t c;
-                    if (mine(l, v, c)) sm.list[atomicAdd(&sm.listed, 1)] = c;
-                });
-                __syncthreads();
-                if (tid < 64) {
-                    const uint64_t c = tid < (int)n ? sm.list[tid] : ~0ull;
-                    const uint64_t w = tid < (int)n && q.weigh ? weight(q, sm.tab, key_value((uint32_t)(c >> 32))) : 0;
-                    uint32_t cs = base_c;
-                    uint64_t ws = base_w;
-                    for (int j = 0; j < (int)n; ++j) {
-                        const uint64_t cj = __shfl(c, j, 64), wj = __shfl(w, j, 64);
-                        if (cj <= c) {
-                            ++cs;
-                            ws += wj;
-                        }
-                    }
-                    if (tid < (int)n && (count ? cs == bound : (ws >= bound && ws - w < bound))) {
-                        sm.at = c;
-                        sm.base_c = cs;
-                        sm.base_w = ws;
-                    }
-                }
-                __syncthreads();
-            };
-            if (k > 0 && (uint32_t)k < kept_c) {
-                search(true, (uint64_t)k);
-                cut = sm.at;
-                kept_c = sm.base_c;
-                kept_w = sm.base_w;
-                __syncthreads();
-            }
-            if (p < 1.f) {
-                const uint64_t bound = (uint64_t)ceil((double)p * (double)kept_w);
-                search(false, bound > 0 ? bound : 1);
-                cut = sm.at;
-                kept_c = sm.base_c;
-                kept_w = sm.base_w;
-                __syncthreads();
-            }
-            if (DRAW) {
-                const uint32_t word = a.noise ? a.noise[i] : counter_word(a.seed, STREAM_TOKEN, a.step, a.row0 + (uint32_t)i, 0);
-                const double u = ((double)word + 0.5) * 0x1p-32;
-                search(false, (uint64_t)(u * (double)kept_w) + 1);
-                if (tid == 0) {
-                    const double x = ((double)key_value((uint32_t)(sm.at >> 32)) - (double)q.top) / (double)t;
-                    a.z[i] = (int32_t)(uint32_t)sm.at;
-                    if (a.logp) a.logp[i] = (float)(x - log(ldexp((double)kept_w, -q.frac)));
-                    if (a.kept) a.kept[i] = (int32_t)kept_c;
-                }
-                continue;
-            }
-        }
-        if constexpr (!DRAW) {
-            if (a.kept && tid == 0) a.kept[i] = (int32_t)kept_c;
-            T* out = (T*)a.out + (int64_t)r * a.ld;
-            const float last = key_value((uint32_t)(cut >> 32));
-            const int last_v = (int)(uint32_t)cut;
-            const bool all = cut == ~0ull;
-            const float largest = sizeof(T) == 2 ? 0x1.FEp127f : FLT_MAX;   // (quotients do not become infinite)
-            auto edit = [&](float l, int v) {
-                const bool stays = l >= q.least && (all || l > last || (l == last && v <= last_v));
-                return stays ? (t == 0.f ? l : fminf(fmaxf(l / t, -largest), largest)) : -INFINITY;
-            };
-            auto store = [&](int c, const uint4& u) {
-                const int v = (c * NT + tid) * E;
-                if (v >= a.V) return;
-                float x[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = edit(Elem<T>::get(u, e), v + e);
-                if (v + E <= a.V) {
-                    if constexpr (sizeof(T) == 2)
-                        *(uint4*)(out + v) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-                    else
-                        *(float4*)(out + v) = make_float4(x[0], x[1], x[2], x[3]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        if (v + e >= a.V) continue;
-                        if constexpr (sizeof(T) == 2) out[v + e] = f32_to_bf16(x[e]);
-                        else out[v + e] = x[e];
-                    }
-                }
-            };
-            if constexpr (RES > 0) {
-#pragma unroll
-                for (int c = 0; c < RES; ++c) store(c, reg[c]);
-            } else {
-                for (int c = 0; c < chunks; ++c) store(c, chunk(c));
-            }
-        }
-    }
 }
 
 // ---------------------------------------------------------------- bf16 rows
@@ -655,7 +284,7 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
         return;
     }
     const float top = key_float(kx);
-    const RowScale q = {top, 0.f, 0.f, TAB * 1.4426950408889634 / (double)t, a.frac, DRAW || p < 1.f};
+    const RowScale q = {top, 0.f, TAB * 1.4426950408889634 / (double)t, a.frac, DRAW || p < 1.f};
     const bool few = kmin > -KMAX;       // (top-k has said so: most numbers do not count)
     int mags;                    // the largest magnitude that can matter
     {
@@ -1051,29 +680,38 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
         constexpr float largest = 0x1.FEp127f;     // (quotients do not become infinite)
         const bool divide = t != 1.f && t != 0.f, fast = quotient_fits(t, top, key_float(last));
         const float rt = 1.f / t;
-        uint32_t some = 0;                         // chunks in which something stays
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            s16x2 x = key[4 * c];
-#pragma unroll
-            for (int y = 1; y < 4; ++y) x = __builtin_elementwise_max(x, key[4 * c + y]);
-            some |= (uint32_t)(max((int)x[0], (int)x[1]) >= last) << c;
-        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int v = (c * NT + tid) * 8;
             if (v >= a.V) continue;
             uint4 o = Elem<bf16_t>::NEG_INF4;
-            if (some >> c & 1) {
-                float f[8];
+            s16x2 x = key[4 * c];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int g = key[4 * c + e / 2][e & 1];
-                    float l = key_float(g);
-                    if (divide) l = fast ? quotient(l, t, rt) : fminf(fmaxf(l / t, -largest), largest);
-                    f[e] = g > last || (g == last && v + e <= last_v) ? l : -INFINITY;
+            for (int y = 1; y < 4; ++y) x = __builtin_elementwise_max(x, key[4 * c + y]);
+            if (max((int)x[0], (int)x[1]) >= last) {
+                // keys above `under` stay; with equal ones up to last_v: whole chunks of them, or one by one
+                const bool split = v <= last_v && last_v < v + 7;
+                const s16x2 under = (s16x2)(short)(v > last_v ? last : last - 1);
+                uint32_t w[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const s16x2 g = key[4 * c + y], sign = g >> (short)15;
+                    // the number's bits, from its key
+                    uint32_t l = __builtin_bit_cast(uint32_t, (s16x2)((g ^ sign) - sign)) | (__builtin_bit_cast(uint32_t, sign) & 0x80008000u);
+                    if (divide) {
+                        const float lo = bf16_lo(l), hi = bf16_hi(l);
+                        l = fast ? pack_bf16x2(quotient(lo, t, rt), quotient(hi, t, rt))
+                                 : pack_bf16x2(fminf(fmaxf(lo / t, -largest), largest), fminf(fmaxf(hi / t, -largest), largest));
+                    }
+                    const uint32_t stays = __builtin_bit_cast(uint32_t, (s16x2)(__builtin_elementwise_sub_sat(under, g) >> (short)15));
+                    w[y] = (l & stays) | (0xFF80FF80u & ~stays);
                 }
-                o = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+                if (split)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((int)key[4 * c + e / 2][e & 1] == last && v + e > last_v)
+                            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | 0xFF800000u : (w[e / 2] & 0xFFFF0000u) | 0xFF80u;
+                o = make_uint4(w[0], w[1], w[2], w[3]);
             }
             if (v + 8 <= a.V) {
                 *(uint4*)(out + v) = o;
@@ -1082,6 +720,512 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (v + e < a.V) out[v + e] = (bf16_t)(w[e / 2] >> (16 * (e & 1)));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- fp32 rows, and bf16 rows of very many classes
+//
+// Every pass reads the row again, from L2 after the first.  (With the row in registers, 52 of them, the compiler keeps
+// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 65.)  Bins are steps of the exponential's table, so a
+// number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
+// of the bin where a bound lies are listed with their weights, and each sums those before it.  Draws that follow each
+// other from one row under the same settings share all but the last step.
+template <int NT>
+struct StreamLds {
+    static constexpr int NW = NT / 64;
+    static constexpr int LOG = NT >= 512 ? 0 : 2;              // steps of the table per bin: 2^LOG
+    static constexpr int BINS = 4096 >> LOG, PARTS = NT;       // bins, and parts that one of them is cut into
+    static constexpr int CANDS = NT / 2;                       // numbers of a bin and its edges that are ordered one by one
+    double tab[TAB];
+    // of the bins; numbers that do not count go behind them, lane by lane
+    uint64_t w1[BINS + 64], w2[PARTS];
+    uint32_t c1[BINS + 64], c2[PARTS];
+    uint64_t place[CANDS], w[CANDS];
+    float value[CANDS];
+    int id[CANDS];
+    uint64_t lo[NW], hi[NW], wsum[NW];
+    uint32_t csum[NW];
+    float mx[NW], kth[NW];
+    uint32_t big[NW];
+    uint64_t before_w, in_w, at;
+    uint32_t before_c, in_c, count;
+    int bin, listed;
+};
+
+// sums before this thread's share and in all, of shares c and w
+template <int NT, typename L>
+DD_DEV void block_scan(L& sm, uint32_t c, uint64_t w, uint32_t& c_at, uint64_t& w_at, uint32_t& c_all, uint64_t& w_all) {
+    constexpr int NW = NT / 64;
+    const int lane = threadIdx.x & 63, wv = same((int)threadIdx.x >> 6);
+    uint32_t ci = c;
+    uint64_t wi = w;
+    wave_scan(ci, wi);
+    if (lane == 63) {
+        sm.csum[wv] = ci;
+        sm.wsum[wv] = wi;
+    }
+    __syncthreads();
+    uint32_t ct = lane < NW ? sm.csum[lane & (NW - 1)] : 0;
+    uint64_t wt = lane < NW ? sm.wsum[lane & (NW - 1)] : 0;
+    const uint32_t c0 = ct;
+    const uint64_t w0 = wt;
+    wave_scan(ct, wt);
+    c_all = of_lane(ct, 63);
+    w_all = of_lane(wt, 63);
+    c_at = ci - c + of_lane(ct, wv) - of_lane(c0, wv);
+    w_at = wi - w + of_lane(wt, wv) - of_lane(w0, wv);
+}
+
+template <typename T, int NT, bool DRAW>
+__global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
+    using L = StreamLds<NT>;
+    constexpr int E = Elem<T>::E, NW = L::NW, BINS = L::BINS, PARTS = L::PARTS, CANDS = L::CANDS, PER = BINS / NT;
+    __shared__ __attribute__((aligned(16))) L sm;
+    const int tid = threadIdx.x, lane = tid & 63, wv = same(tid >> 6);
+    const int chunks = (a.V + NT * E - 1) / (NT * E);
+    if (tid < TAB) sm.tab[tid] = power_table.v[tid];
+    // of the row whose sums stand in LDS
+    int have_row = -1, have_set = -1, state = 0;      // state: 0 the first class alone, 1 no choice, 2 sums
+    RowScale q = {};
+    float t = 1.f;
+    bool weigh = false, counted = false;
+    uint64_t kept_w = 0, cut = ~0ull, w_at = 0, w_sum = 0;
+    uint32_t kept_c = 0, c_at = 0, c_sum = 0;
+    const int i0 = blockIdx.x * a.chunk, i1 = min(i0 + a.chunk, a.n);
+    for (int i = i0; i < i1; ++i) {
+        int r = i;
+        if (DRAW && a.row_ids) {
+            r = a.row_ids[i];
+            if (r < 0 || r >= a.rows) {
+                if (r != -1 && tid == 0 && a.err) atomicOr(a.err, DD_DEVERR_SAMPLING);
+                continue;
+            }
+        }
+        const int set = i / a.per;
+        const T* row = (const T*)a.logits + (int64_t)r * a.ld;
+        // f(numbers, class of the first) for each chunk; what stands behind the row is -inf
+        auto each_chunk = [&](auto&& f) {
+            constexpr int AHEAD = 4;       // chunks whose loads are under way together
+            for (int c0 = 0; c0 < chunks; c0 += AHEAD) {
+                uint4 u[AHEAD];
+#pragma unroll
+                for (int c = 0; c < AHEAD; ++c)      // (no branch between the loads; ld is a multiple of 8: in bounds)
+                    u[c] = *(const uint4*)(row + min(((c0 + c) * NT + tid) * E, (a.V - 1) & ~(E - 1)));
+#pragma unroll
+                for (int c = 0; c < AHEAD; ++c) {
+                    const int v = ((c0 + c) * NT + tid) * E;
+                    if (c0 + c >= chunks) break;
+                    if (v >= a.V) u[c] = Elem<T>::NEG_INF4;
+                    else if (v + E > a.V) Elem<T>::clip(u[c], a.V - v);
+                    float x[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = Elem<T>::get(u[c], e);
+                    f(x, v);
+                }
+            }
+        };
+        // bin and weight of a number: of t = turn (top - x) the nearest whole step, from the last bits of t + 1.5 2^52, and as in weight()
+        auto weight_of = [&](float x, int& bin) -> uint64_t {
+            const double u = fmin(((double)q.top - (double)x) * q.turn, (double)(64 * TAB - 1));
+            const double m = u + 0x1.8p52, f = (m - 0x1.8p52) - u;
+            const int n = (int)(uint32_t)__double_as_longlong(m);
+            constexpr double s = 0.69314718055994530942 / TAB;
+            double e = fma(f, s * s * s * s * s / 120.0, s * s * s * s / 24.0);
+            e = fma(f, e, s * s * s / 6.0);
+            e = fma(f, e, s * s / 2.0);
+            e = fma(f, e, s);
+            e = fma(f, e, 1.0);
+            e = ldexp(e * sm.tab[n & (TAB - 1)], q.frac - n / TAB);
+            bin = n >> L::LOG;
+            return (uint64_t)__double_as_longlong(e + 0x1p52) - 0x4330000000000000ull;
+        };
+        static_assert(BINS << L::LOG == 64 * TAB, "bins end where weights do");
+        uint64_t at = 0;
+        int step = 2;                      // top-k, top-p, draw
+        int k = 0;
+        float p = 1.f;
+        if (r != have_row || set != have_set) {
+            have_row = r;
+            have_set = set;
+            t = a.temperature ? a.temperature[set] : 1.f;
+            p = a.top_p ? a.top_p[set] : 1.f;
+            const float m = a.min_p ? a.min_p[set] : 0.f;
+            k = a.top_k ? a.top_k[set] : 0;
+            float mx = -INFINITY, kth = -INFINITY;
+            uint32_t big = 0;              // NaN stands above infinity
+            each_chunk([&](const float (&x)[E], int) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    mx = fmaxf(mx, x[e]);
+                    big = max(big, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+                }
+            });
+            if (k > 1 && k <= NT) {        // (as for bf16 rows)
+                const int rank = (k + NW - 1) / NW;
+                const uint32_t mine = ~value_key(mx);
+                uint32_t found = 0;
+                for (int b = 31; b >= 0; --b)
+                    if (__popcll(__ballot(mine >= (found | 1u << b))) >= rank) found |= 1u << b;
+                kth = key_value(~found);
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+                big = max(big, (uint32_t)__shfl_xor((int)big, o, 64));
+            }
+            __syncthreads();               // the last row's sums
+            if (lane == 0) {
+                sm.mx[wv] = mx;
+                sm.kth[wv] = kth;
+                sm.big[wv] = big;
+            }
+            for (int b = tid; b < BINS / 2; b += NT) ((uint4*)sm.w1)[b] = make_uint4(0u, 0u, 0u, 0u);
+            for (int b = tid; b < BINS / 4; b += NT) ((uint4*)sm.c1)[b] = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+            mx = sm.mx[lane & (NW - 1)];
+            kth = sm.kth[lane & (NW - 1)];
+            big = sm.big[lane & (NW - 1)];
+#pragma unroll
+            for (int o = NW / 2; o > 0; o >>= 1) {
+                mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+                kth = fminf(kth, __shfl_xor(kth, o, 64));
+                big = max(big, (uint32_t)__shfl_xor((int)big, o, 64));
+            }
+            mx = __int_as_float(same(__float_as_int(mx)));
+            kth = __int_as_float(same(__float_as_int(kth)));
+            big = same(big);
+            const bool settings = t >= 0.f && t < INFINITY && p >= 0.f && m >= 0.f && m <= 1.f;   // (false for NaN)
+            if (big > 0x7F800000u || mx == INFINITY || mx == -INFINITY || !settings) {
+                state = 1;
+                if (tid == 0 && a.err) atomicOr(a.err, settings ? DD_DEVERR_LOGITS : DD_DEVERR_SAMPLING);
+            } else {
+                state = t == 0.f || k == 1 ? 0 : 2;
+                q = {mx, fmaxf(kth, -FLT_MAX), TAB * 1.4426950408889634 / (double)t, a.frac, true};
+                if (m > 0.f && t > 0.f) {  // w >= m where l >= top + t log m
+                    const double b = (double)mx + (double)t * log((double)m);
+                    if (b > -FLT_MAX) {
+                        float f = (float)b;
+                        if ((double)f < b) f = key_value(value_key(f) - 1);     // the next number above
+                        q.least = fmaxf(q.least, f);
+                    }
+                }
+                cut = ~0ull;
+                kept_c = 0;
+                counted = false;
+                if (state == 0) {          // the lowest index of the largest number
+                    if (tid == 0) sm.bin = INT_MAX;
+                    __syncthreads();
+                    int v = INT_MAX;
+                    each_chunk([&](const float (&x)[E], int at) {
+#pragma unroll
+                        for (int e = E - 1; e >= 0; --e)
+                            if (x[e] == mx) v = min(v, at + e);
+                    });
+                    if (v != INT_MAX) atomicMin(&sm.bin, v);
+                    __syncthreads();
+                    cut = place(mx, same(sm.bin));
+                    kept_c = 1;
+                    counted = true;
+                }
+                weigh = DRAW || p < 1.f;
+                if (state == 2 && (weigh || k > 0)) {
+                    const bool few = kth > -INFINITY;
+                    each_chunk([&](const float (&x)[E], int) {
+                        bool any = false;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) any |= x[e] >= q.least;
+                        if (few && !__any(any)) return;
+#pragma unroll
+                        for (int h = 0; h < E; h += 4) {
+                            int bin[4];
+                            uint64_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                w[e] = weight_of(x[h + e], bin[e]);
+                                bin[e] = x[h + e] >= q.least ? bin[e] : BINS + lane;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                if (weigh) atomicAdd((unsigned long long*)&sm.w1[bin[e]], (unsigned long long)w[e]);
+                                if (k > 0) atomicAdd(&sm.c1[bin[e]], 1u);
+                            }
+                        }
+                    });
+                    __syncthreads();
+                    c_sum = 0;
+                    w_sum = 0;
+#pragma unroll
+                    for (int b = 0; b < PER; ++b) {
+                        c_sum += sm.c1[tid * PER + b];
+                        w_sum += sm.w1[tid * PER + b];
+                    }
+                    block_scan<NT>(sm, c_sum, w_sum, c_at, w_at, kept_c, kept_w);
+                    step = 0;
+                }
+            }
+        }
+        if (state == 1) {
+            if (tid == 0) {
+                if (a.kept) a.kept[i] = 0;
+                if (DRAW) {
+                    a.z[i] = 0;
+                    if (a.logp) a.logp[i] = NAN;
+                }
+            }
+            if (!DRAW && a.out != a.logits) {
+                T* out = (T*)a.out + (int64_t)r * a.ld;
+                for (int v = tid; v < a.V; v += NT) out[v] = row[v];
+            }
+            continue;
+        }
+        if (state == 2 && (DRAW || step == 0)) {
+            for (; step < (DRAW ? 3 : 2); ++step) {
+                bool count = false;
+                uint64_t bound = 0;
+                if (step == 0) {
+                    if (!(k > 0 && (uint32_t)k < kept_c)) continue;
+                    count = true;
+                    bound = (uint32_t)k;
+                } else if (step == 1) {
+                    if (!(p < 1.f)) continue;
+                    bound = same((uint64_t)ceil((double)p * (double)kept_w));
+                    bound = bound > 0 ? bound : 1;
+                } else {
+                    const uint32_t word = a.noise ? a.noise[i] : counter_word(a.seed, STREAM_TOKEN, a.step, a.row0 + (uint32_t)i, 0);
+                    bound = same((uint64_t)(((double)word + 0.5) * 0x1p-32 * (double)kept_w) + 1);
+                }
+                // the bin where the running count or weight reaches the bound
+                if (count ? c_at < bound && bound <= c_at + c_sum : w_at < bound && bound <= w_at + w_sum) {
+                    uint32_t c = c_at;
+                    uint64_t w = w_at;
+#pragma unroll 1
+                    for (int b = tid * PER;; ++b) {
+                        const uint32_t c0 = sm.c1[b];
+                        const uint64_t w0 = sm.w1[b];
+                        if (count ? bound <= c + c0 : bound <= w + w0) {
+                            sm.bin = b;
+                            sm.before_c = c;
+                            sm.before_w = w;
+                            sm.listed = 0;
+                            break;
+                        }
+                        c += c0;
+                        w += w0;
+                    }
+                }
+                __syncthreads();
+                const int bin1 = same(sm.bin);
+                uint32_t base_c = same(sm.before_c);
+                uint64_t base_w = same(sm.before_w);
+                // numbers that may stand in that bin: a quarter of a step more at either side
+                const int n0 = bin1 << L::LOG, n1 = n0 + (1 << L::LOG) - 1;
+                const float from = bin1 == BINS - 1 ? -FLT_MAX : (float)fmax((double)q.top - ((double)n1 + 0.75) / q.turn, -FLT_MAX);
+                const float upto = bin1 == 0 ? q.top : (float)fmax((double)q.top - ((double)n0 - 0.75) / q.turn, -FLT_MAX);
+                const float low = fmaxf(from, q.least), high = fmaxf(upto, low);
+                // (a draw's pass counts what stays, if that is asked for and top-k has not said it)
+                const bool tally = step == 2 && a.kept && !counted;
+                const float last = key_value((uint32_t)(cut >> 32));
+                uint32_t stay = 0;
+                each_chunk([&](const float (&x)[E], int v) {
+                    bool in[E], any = false;
+                    if (tally)
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            stay += x[e] >= q.least && (cut == ~0ull || x[e] > last || (x[e] == last && v + e <= (int)(uint32_t)cut));
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        in[e] = __builtin_amdgcn_fmed3f(x[e], low, high) == x[e];
+                        any |= in[e];
+                    }
+                    if (!__any(any)) return;
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (in[e]) {
+                            const int y = atomicAdd(&sm.listed, 1);
+                            if (y < CANDS) {
+                                sm.value[y] = x[e];
+                                sm.id[y] = v + e;
+                            }
+                        }
+                });
+                if (tally) {
+                    stay = wave_scan(stay);
+                    if (lane == 63) sm.csum[wv] = stay;
+                }
+                __syncthreads();
+                if (tally) {
+                    kept_c = 0;
+                    for (int x = 0; x < NW; ++x) kept_c += same(sm.csum[x]);
+                    counted = true;
+                }
+                int n = same(sm.listed);
+                if (n <= CANDS) {
+                    if (tid < n) {
+                        int bin;
+                        const uint64_t w = weight_of(sm.value[tid], bin);
+                        sm.place[tid] = bin == bin1 ? place(sm.value[tid], sm.id[tid]) : ~0ull;
+                        sm.w[tid] = bin == bin1 && weigh ? w : 0;
+                    }
+                } else {
+                    // too many: their places in PARTS parts, and those of the part where the bound lies, until they are few
+                    uint64_t lo = 0, hi = ~0ull;
+                    auto each = [&](auto&& f) {         // f(place, weight)
+#pragma unroll 1
+                        for (int v = tid; v < a.V; v += NT) {
+                            const float x = Elem<T>::load1(row, v);
+                            if (!(x >= low && x <= high)) continue;
+                            int bin;
+                            const uint64_t w = weight_of(x, bin), at = place(x, v);
+                            if (bin == bin1 && at >= lo && at <= hi) f(at, w);
+                        }
+                    };
+                    do {
+                        uint64_t first = ~0ull, past = 0;
+                        each([&](uint64_t at, uint64_t) {
+                            first = first < at ? first : at;
+                            past = past > at ? past : at;
+                        });
+                        for (int o = 32; o > 0; o >>= 1) {
+                            const uint64_t f = __shfl_xor(first, o, 64), g = __shfl_xor(past, o, 64);
+                            first = first < f ? first : f;
+                            past = past > g ? past : g;
+                        }
+                        if (lane == 0) {
+                            sm.lo[wv] = first;
+                            sm.hi[wv] = past;
+                        }
+                        sm.c2[tid] = 0;
+                        sm.w2[tid] = 0;
+                        __syncthreads();
+                        for (int x = 0; x < NW; ++x) {
+                            first = first < sm.lo[x] ? first : sm.lo[x];
+                            past = past > sm.hi[x] ? past : sm.hi[x];
+                        }
+                        first = same(first);
+                        past = same(past);
+                        int shift = 0;
+                        while (((past - first) >> shift) >= PARTS) ++shift;
+                        each([&](uint64_t at, uint64_t w) {
+                            const int b = (int)((at - first) >> shift);
+                            atomicAdd(&sm.c2[b], 1u);
+                            if (weigh) atomicAdd((unsigned long long*)&sm.w2[b], (unsigned long long)w);
+                        });
+                        __syncthreads();
+                        const uint32_t c = sm.c2[tid];
+                        const uint64_t w = sm.w2[tid];
+                        uint32_t ca, call;
+                        uint64_t wa, wall;
+                        block_scan<NT>(sm, c, w, ca, wa, call, wall);
+                        ca += base_c;
+                        wa += base_w;
+                        if (count ? ca < bound && bound <= ca + c : wa < bound && bound <= wa + w) {
+                            sm.bin = tid;
+                            sm.before_c = ca;
+                            sm.before_w = wa;
+                            sm.in_c = c;
+                            sm.listed = 0;
+                        }
+                        __syncthreads();
+                        base_c = same(sm.before_c);
+                        base_w = same(sm.before_w);
+                        n = (int)same(sm.in_c);
+                        lo = first + ((uint64_t)same(sm.bin) << shift);
+                        hi = lo + ((1ull << shift) - 1);
+                        __syncthreads();
+                    } while (n > CANDS);
+                    each([&](uint64_t at, uint64_t w) {
+                        const int x = atomicAdd(&sm.listed, 1);
+                        sm.place[x] = at;
+                        sm.w[x] = weigh ? w : 0;
+                    });
+                }
+                __syncthreads();
+                if (tid < n) {
+                    const uint64_t mine = sm.place[tid], own = sm.w[tid];
+                    uint32_t cs = base_c;
+                    uint64_t ws = base_w;
+#pragma unroll 4
+                    for (int x = 0; x < n; ++x) {
+                        const bool in = sm.place[x] <= mine;
+                        cs += in;
+                        ws += in ? sm.w[x] : 0;
+                    }
+                    if (mine != ~0ull && (count ? cs == bound : ws >= bound && ws - own < bound)) {
+                        sm.at = mine;
+                        sm.before_c = cs;
+                        sm.before_w = ws;
+                    }
+                }
+                __syncthreads();
+                at = same(sm.at);
+                if (step < 2) {
+                    cut = at;
+                    kept_w = same(sm.before_w);
+                    kept_c = same(sm.before_c);
+                    counted = count;
+                }
+                __syncthreads();
+            }
+        }
+        const float last = key_value((uint32_t)(cut >> 32));
+        const int last_v = (int)(uint32_t)cut;
+        const bool all = cut == ~0ull;
+        auto stays = [&](float x, int v) { return x >= q.least && (all || x > last || (x == last && v <= last_v)); };
+        if (DRAW && tid == 0) {
+            if (a.kept) a.kept[i] = (int32_t)kept_c;
+            if (state == 0) at = cut;
+            a.z[i] = (int32_t)(uint32_t)at;
+            if (a.logp) {
+                const double x = ((double)key_value((uint32_t)(at >> 32)) - (double)q.top) / (double)t;
+                a.logp[i] = state == 0 ? 0.f : (float)(x - log(ldexp((double)kept_w, -q.frac)));
+            }
+        }
+        if constexpr (!DRAW) {
+            T* out = (T*)a.out + (int64_t)r * a.ld;
+            constexpr float largest = sizeof(T) == 2 ? 0x1.FEp127f : FLT_MAX;   // (quotients do not become infinite)
+            const bool divide = t != 1.f && t != 0.f, fast = quotient_fits(t, q.top, all ? q.least : last);
+            const float rt = 1.f / t;
+            uint32_t n = 0;
+            each_chunk([&](const float (&x)[E], int v) {
+                if (v >= a.V) return;
+                float y[E];
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const bool in = stays(x[e], v + e);
+                    n += in;
+                    any |= in;
+                    y[e] = in ? x[e] : -INFINITY;
+                }
+                if (divide && any)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float z = fast ? quotient(x[e], t, rt) : fminf(fmaxf(x[e] / t, -largest), largest);
+                        y[e] = y[e] == -INFINITY ? y[e] : z;
+                    }
+                if (v + E <= a.V) {
+                    if constexpr (sizeof(T) == 2)
+                        *(uint4*)(out + v) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                    else
+                        *(float4*)(out + v) = make_float4(y[0], y[1], y[2], y[3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        if (v + e >= a.V) continue;
+                        if constexpr (sizeof(T) == 2) out[v + e] = f32_to_bf16(y[e]);
+                        else out[v + e] = y[e];
+                    }
+                }
+            });
+            if (a.kept) {
+                n = wave_scan(n);
+                if (tid == 0) sm.count = 0;
+                __syncthreads();
+                if (lane == 63) atomicAdd(&sm.count, n);
+                __syncthreads();
+                if (tid == 0) a.kept[i] = (int32_t)sm.count;
             }
         }
     }
@@ -1106,12 +1250,18 @@ static void launch_sample_keys(const SampleArgs& a, hipStream_t s) {
 }
 
 template <typename T, bool DRAW>
-static void launch_sample_t(const SampleArgs& a, hipStream_t s) {
+static void launch_sample_t(const SampleArgs& args, hipStream_t s) {
+    SampleArgs a = args;
     if constexpr (sizeof(T) == 2) {
         if (a.V <= 131072 && grid_fits(a.n, 1024)) return launch_sample_keys<DRAW>(a, s);
     }
-    const dim3 grid((unsigned)std::min<int64_t>(a.n, 2 * num_cus()));
-    launch_k((sample_kernel<T, 1024, 0, DRAW>), grid, dim3(1024), 0, s, a);
+    // Draws that share a row and its settings are one workgroup's as far as every CU has one.
+    a.chunk = DRAW && a.per > 1 ? (int)std::max<int64_t>(1, a.n / num_cus()) : 1;
+    if (!grid_fits(ceil_div(a.n, a.chunk), 1024)) a.chunk = 1024;
+    auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)ceil_div(a.n, a.chunk)), dim3(threads), 0, s, a); };
+    if (a.V <= 4096) return go(sample_stream_kernel<T, 256, DRAW>, 256);
+    if (ceil_div(a.n, a.chunk) > num_cus()) return go(sample_stream_kernel<T, 512, DRAW>, 512);
+    go(sample_stream_kernel<T, 1024, DRAW>, 1024);
 }
 
 dd_status launch_sample(const SampleArgs& args, int dtype, bool draw, hipStream_t s) {

@@ -173,7 +173,7 @@ struct SampleArgs {
     float* logp;
     void* out;
     int32_t *kept, *err;
-    int frac;                 // set by launch_sample
+    int frac, chunk;          // set by launch_sample: weights are multiples of 2^-frac; draws of a workgroup
 };
 dd_status launch_sample(const SampleArgs& a, int logits_dtype, bool draw, hipStream_t s);
 dd_status launch_latent(const int32_t* x, int32_t rows, int32_t V, double at, double sigma,
