@@ -92,8 +92,10 @@ struct CacheAttnPlan {
 CacheAttnPlan cache_attn_plan(int32_t S, int32_t T, int32_t Hkv, int32_t Hq, int dh, int32_t max_new, int32_t max_kv);
 dd_status launch_cache_attn(int dtype, const CacheAttnArgs& a, const CacheAttnPlan& p, hipStream_t s);
 
-// Ranges of blocks that a fork or a compaction cuts the pool into (n_blocks is below 2^26).
+// Ranges of blocks that a fork or a compaction cuts the pool into (n_blocks is below 2^26), and parts of the sequences: as
+// many as give every CU something to do.
 constexpr int PAGE_RANGE = 8192, PAGE_RANGES = (1 << 26) / PAGE_RANGE;
+inline int page_parts(int ranges) { return ranges >= 256 ? 1 : 256 / ranges < 32 ? 256 / ranges : 32; }
 
 struct ForkArgs {
     CacheShape c;
@@ -103,12 +105,13 @@ struct ForkArgs {
     int32_t* free_blocks;
     const int32_t* n_free;
     int32_t *n_free_out, *moves, *n_moves;
-    // workspace: a bit per block that is freed, their number in each range, whether a sequence takes a fresh block, whether
-    // an input is no fork's
-    uint32_t* freed;
+    // workspace: bits per block and part, held by old sequences and whole by new ones; a bit per block that is freed, their
+    // number in each range; whether a sequence takes a fresh block; whether an input of a part is no fork's
+    uint32_t *old, *whole, *freed;
     int32_t *counts, *copies, *bad;
     int32_t ranges;
     int32_t* err;
+    int32_t parts;       // set by launch_cache_fork
 };
 dd_status launch_cache_fork(const ForkArgs& a, hipStream_t s);
 
@@ -117,12 +120,13 @@ struct CompactArgs {
     int32_t S, ld_table;
     const int32_t *table, *held;
     int32_t *to_table, *free_blocks, *n_free_out, *moves, *n_moves;
-    // workspace: a bit per block in use, those of the range before each word of them, those of each range, whether an
-    // input is no table
+    // workspace: a bit per block in use and part, later in all; those of the range before each word of them; those of each
+    // range; whether an input of a part is no table
     uint32_t* used;
     int32_t *before, *counts, *bad;
     int32_t ranges;
     int32_t* err;
+    int32_t parts;       // set by launch_cache_compact
 };
 dd_status launch_cache_compact(const CompactArgs& a, hipStream_t s);
 

@@ -1122,17 +1122,19 @@ dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t l
 
 // ---------------------------------------------------------------- blocks between passes
 
+// Offsets in the workspace of a fork (bits of two kinds per part, `copies` numbers) or a compaction (one kind).
 struct PageWs {
-    size_t bits, before, counts, copies, total;
+    size_t bits, more, words, counts, copies, total;
     int32_t ranges;
 };
-static PageWs page_ws(const dd_cache* c, int64_t copies, bool before) {
+static PageWs page_ws(const dd_cache* c, int kinds, int64_t copies) {
     PageWs w;
     w.ranges = (int32_t)ceil_div(c->n_blocks, PAGE_RANGE);
-    const size_t words = align256(4 * (size_t)ceil_div(c->n_blocks, 32));
-    w.bits = 256;                       // (the first word says whether an input does not fit)
-    w.before = w.bits + words;
-    w.counts = w.before + (before ? words : 0);
+    const size_t words = 4 * (size_t)ceil_div(c->n_blocks, 32), part = align256((size_t)page_parts(w.ranges) * words);
+    w.bits = 256;                       // (the first words say whether an input of a part does not fit)
+    w.more = w.bits + part;
+    w.words = w.bits + kinds * part;
+    w.counts = w.words + align256(words);
     w.copies = w.counts + align256(4 * (size_t)w.ranges);
     w.total = w.copies + align256(4 * (size_t)copies);
     return w;
@@ -1151,7 +1153,7 @@ static dd_status pages_map_check(const dd_cache* cache, const dd_cache_map* m) {
 
 size_t dd_cache_fork_workspace_bytes(const dd_cache* cache, int32_t S, int32_t S_to) {
     if (cache_check(cache) != DD_OK || S < 0 || S > (1 << 16) || S_to < 0 || S_to > (1 << 16)) return 0;
-    return page_ws(cache, S_to, false).total;
+    return page_ws(cache, 2, S_to).total;
 }
 
 dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd_cache_map* to, const int32_t* seq_len,
@@ -1166,19 +1168,20 @@ dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd
     DD_CHECK(map->S == 0 || to->S == 0 || (map->block_table != to->block_table && map->held != to->held &&
                                            map->kv_len != to->kv_len && seq_len != to->kv_len),
              DD_E_ARG, "the new tables and lengths must be other arrays than the old ones");
-    const PageWs w = page_ws(cache, to->S, false);
+    const PageWs w = page_ws(cache, 2, to->S);
     DD_CHECK(ws && ((uintptr_t)ws & 255) == 0, DD_E_ARG, "ws must be a 256-byte aligned buffer");
     DD_CHECK(ws_bytes >= w.total, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, w.total);
     char* b = (char*)ws;
     ForkArgs a = {cache_shape(cache), map->S, to->S, map->ld_table, to->ld_table, map->block_table, map->held, seq_len, src,
                   keep, to->block_table, to->held, to->kv_len, free_blocks, n_free, n_free_out, moves, n_moves,
-                  (uint32_t*)(b + w.bits), (int32_t*)(b + w.counts), (int32_t*)(b + w.copies), (int32_t*)b, w.ranges, dev_err};
+                  (uint32_t*)(b + w.bits), (uint32_t*)(b + w.more), (uint32_t*)(b + w.words), (int32_t*)(b + w.counts),
+                  (int32_t*)(b + w.copies), (int32_t*)b, w.ranges, dev_err, 1};
     return launch_cache_fork(a, (hipStream_t)stream);
 }
 
 size_t dd_cache_compact_workspace_bytes(const dd_cache* cache) {
     if (cache_check(cache) != DD_OK) return 0;
-    return page_ws(cache, 0, true).total;
+    return page_ws(cache, 1, 0).total;
 }
 
 dd_status dd_cache_compact(const dd_cache* cache, const dd_cache_map* map, int32_t* block_table_out, int32_t* free_blocks,
@@ -1187,13 +1190,13 @@ dd_status dd_cache_compact(const dd_cache* cache, const dd_cache_map* map, int32
     DD_TRY(pages_map_check(cache, map));
     DD_CHECK((map->S == 0 || block_table_out) && free_blocks && n_free_out && n_moves && (moves || cache->n_blocks == 1),
              DD_E_ARG, "NULL pointer argument");
-    const PageWs w = page_ws(cache, 0, true);
+    const PageWs w = page_ws(cache, 1, 0);
     DD_CHECK(ws && ((uintptr_t)ws & 255) == 0, DD_E_ARG, "ws must be a 256-byte aligned buffer");
     DD_CHECK(ws_bytes >= w.total, DD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, w.total);
     char* b = (char*)ws;
     CompactArgs a = {cache_shape(cache), map->S, map->ld_table, map->block_table, map->held, block_table_out, free_blocks,
-                     n_free_out, moves, n_moves, (uint32_t*)(b + w.bits), (int32_t*)(b + w.before), (int32_t*)(b + w.counts),
-                     (int32_t*)b, w.ranges, dev_err};
+                     n_free_out, moves, n_moves, (uint32_t*)(b + w.bits), (int32_t*)(b + w.words), (int32_t*)(b + w.counts),
+                     (int32_t*)b, w.ranges, dev_err, 1};
     return launch_cache_compact(a, (hipStream_t)stream);
 }
 

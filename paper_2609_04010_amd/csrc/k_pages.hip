@@ -1,10 +1,11 @@
 // Blocks of the cached context between passes: contexts that go on in several sequences, blocks copied, a pool put in
 // order.
 //
-// Fork and compaction ask, for every block of the pool, which sequences hold it.  Launch 1 cuts the pool into ranges of
-// RB blocks, one workgroup each: every workgroup walks all tables and keeps what falls into its range in LDS, so
-// nothing has to be cleared first and no atomics leave the CU; it leaves a bit per block and a count per range.  Launch 2
-// ranks blocks by those counts and the bits, and writes tables, stack and moves.
+// Fork and compaction ask, for every block of the pool, which sequences hold it.  The pool is cut into ranges of RB blocks and
+// the sequences into up to page_parts() parts: a workgroup of the first launch walks the tables of one part and keeps what falls
+// into one range as bits in LDS, so nothing has to be cleared first and no atomics leave the CU.  The second launch joins
+// the parts of each range and counts; the others rank blocks by those counts and write tables, stack and moves.  Bound by
+// latency and launches: a pool of one range and few sequences is one launch.
 #include <algorithm>
 
 #include "cache.h"
@@ -15,38 +16,45 @@ namespace {
 
 constexpr int RB = PAGE_RANGE;      // blocks of a range
 constexpr int RW = RB / 32;         // words of its bits
-constexpr int MT = 1024;            // threads of launch 1
-constexpr int AT = 256;             // threads of launch 2
+constexpr int MT = 1024;            // threads of the launches that look at ranges
+constexpr int AT = 256;             // threads of the others
 static_assert(RW == AT, "a thread per word of a range");
+constexpr int SOURCES = 8192;       // old rows up to which LDS holds how much of them stays
 
-// f(block, row, j, length) for entry j < length of every row; head(row, source, length) says where a row stands in
-// the table.  A wavefront takes whole rows, the heads of 64 at once and the first entries of four.
-template <int NT, typename Head, typename F>
-DD_DEV void walk(const int32_t* table, int64_t ld, int rows, Head&& head, F&& f) {
+// f(block, j, head) for entry j < head.len of the rows part, part + parts, .. (block -1 behind that: no branch per lane); head(row)
+// says how long a row is, and what else f wants to know.  A wavefront takes whole rows: the heads of 64 at once, then 256
+// entries at a time.  Short code on purpose: each wavefront passes here a few times only, and fetching the instructions is
+// most of that (32 rows on their way together, unrolled, took 17 us for 1024 rows of 128 in 8 parts;
+// this takes 7, in 16).
+struct Head {
+    int len, whole;
+};
+template <int NT, typename H, typename F>
+DD_DEV void walk(const int32_t* table, int64_t ld, int all, int part, int parts, H&& head, F&& f) {
     constexpr int W = NT / 64;
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = (all - part + parts - 1) / parts;
+#pragma unroll 1
     for (int base = wv; base < rows; base += 64 * W) {
-        int src = 0, len = 0;
-        if (base + lane * W < rows) head(base + lane * W, src, len);
-        for (int g = 0; g < 64 && base + g * W < rows; g += 4) {
-            const int32_t* p[4];
-            int n[4], b[4];
+        Head mine = {0, 0};
+        if (base + lane * W < rows) mine = head((base + lane * W) * parts + part);
+#pragma unroll 1
+        for (int g = 0; g < 64 && base + g * W < rows; ++g) {
+            const Head h = {__builtin_amdgcn_readlane(mine.len, g), __builtin_amdgcn_readlane(mine.whole, g)};
+            const int32_t* p = table + ((int64_t)(base + g * W) * parts + part) * ld;
+#pragma unroll 1
+            for (int j0 = lane; j0 - lane < h.len; j0 += 256) {
+                int b[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                n[u] = __builtin_amdgcn_readlane(len, g + u);
-                p[u] = table + (int64_t)__builtin_amdgcn_readlane(src, g + u) * ld;
-                b[u] = lane < n[u] ? p[u][lane] : 0;
-            }
+                for (int u = 0; u < 4; ++u) b[u] = p[min(j0 + 64 * u, h.len - 1)];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int row = base + (g + u) * W;
-                if (lane < n[u]) f(b[u], row, lane, n[u]);
-#pragma unroll 4
-                for (int j = lane + 64; j < n[u]; j += 64) f(p[u][j], row, j, n[u]);
+                for (int u = 0; u < 4; ++u) f(j0 + 64 * u < h.len ? b[u] : -1, j0 + 64 * u, h);
             }
         }
     }
 }
+// whether an entry is out of range: entries of -1 that stand in a table are told from those behind a row by their place
+DD_DEV bool wrong(int b, int j, const Head& h, int n_blocks) { return (uint32_t)b >= (uint32_t)n_blocks && j < h.len; }
 
 // where row s of the new tables comes from, and how many entries it has; false where that is no fork's
 DD_DEV bool fork_head(const ForkArgs& a, int s, int& src, int& len, int& keep) {
@@ -112,69 +120,118 @@ DD_DEV int nth_bit(uint32_t w, int r) {
 //
 // Row s of the new tables is the first ceil(keep_s / P) entries of row src_s of the old ones.  A block is freed if an old
 // row holds it and no new one.  owner[b]: -1 where a new row holds b whole, else the first sequence whose partly filled last
-// block it is; the other sequences of that kind take a fresh block, and a move for its contents.
-__global__ __launch_bounds__(MT) void fork_mark_kernel(ForkArgs a) {
-    __shared__ int32_t owner[RB];
-    __shared__ uint32_t old[RW];
-    __shared__ int red[MT / 64], bad;
-    const int tid = threadIdx.x, b0 = blockIdx.x * RB;
-    const bool first = blockIdx.x == 0;
-    for (int i = tid; i < RB; i += MT) owner[i] = INT32_MAX;
-    if (tid < RW) old[tid] = 0;
-    if (tid == 0) bad = 0;
+// block it is; the other sequences of that kind take a fresh block, and a move for its contents.  What is held whole of an old row
+// is a beginning of it, the longest that any new row asks for: the new rows are not walked.  1024
+// rows of 65 entries, 10 ranges: 6 us with 25 parts, 12 with 8, 19 with one.
+struct ForkLds {
+    int32_t owner[RB];
+    uint32_t old[RW], whole[RW], last[RW];      // held by an old row; whole by a new one; as a new one's partly filled last
+    int32_t most[SOURCES];                      // whole blocks of an old row that new rows hold
+    int red[MT / 64], bad;
+};
+
+DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
+    const int tid = threadIdx.x, b0 = range * RB;
+    const bool first = range == 0, fits = a.S <= SOURCES;
+    for (int i = tid; i < (fits ? a.S : 0); i += MT) sm.most[i] = 0;
+    if (tid < RW) sm.old[tid] = sm.whole[tid] = 0;
+    if (tid == 0) sm.bad = 0;
     __syncthreads();
-    walk<MT>(a.table, a.ld_table, a.S,
-             [&](int q, int& src, int& len) {
-                 src = q;
-                 bool ok = held_ok(a.held, a.ld_table, q, len);
+    bool bad = false;
+    for (int s = tid; s < a.S_to; s += MT) {
+        int src, len, keep;
+        bad |= !fork_head(a, s, src, len, keep);
+        const int n = keep >> a.c.log2p;
+        if (fits && n > 0) atomicMax(&sm.most[src], n);
+    }
+    __syncthreads();
+    walk<MT>(a.table, a.ld_table, a.S, part, a.parts,
+             [&](int q) {
+                 int len;
+                 bad |= !held_ok(a.held, a.ld_table, q, len);
                  if (first) {
                      const int have = a.seq_len[q];
-                     ok = ok && have >= 0 && have <= (int64_t)len * a.c.P;
+                     bad |= have < 0 || have > (int64_t)len * a.c.P;
                  }
-                 if (!ok) bad = 1;
+                 return Head{len, fits ? sm.most[q] : 0};
              },
-             [&](int b, int, int, int) {
-                 if (b < 0 || b >= a.c.n_blocks) bad = 1;
+             [&](int b, int j, const Head& h) {
+                 if (first) bad |= wrong(b, j, h, a.c.n_blocks);      // (one range's workgroups look)
                  const uint32_t x = (uint32_t)b - (uint32_t)b0;
-                 if (x < RB) atomicOr(&old[x >> 5], 1u << (x & 31));
+                 if (x < RB) {
+                     atomicOr(&sm.old[x >> 5], 1u << (x & 31));
+                     if (j < h.whole) atomicOr(&sm.whole[x >> 5], 1u << (x & 31));
+                 }
              });
-    walk<MT>(a.table, a.ld_table, a.S_to,
-             [&](int s, int& src, int& len) {
-                 int keep;
-                 if (!fork_head(a, s, src, len, keep)) bad = 1;
-             },
-             [&](int b, int s, int j, int n) {
-                 const uint32_t x = (uint32_t)b - (uint32_t)b0;
-                 if (x >= RB) return;
-                 int who = -1;
-                 if (j == n - 1 && ((a.keep ? a.keep[s] : a.seq_len[a.src[s]]) & (a.c.P - 1))) who = s;   // partly filled
-                 atomicMin(&owner[x], who);
-             });
-    __syncthreads();
-    int n = 0;
-    if (tid < RW) {
-        uint32_t w = old[tid];
-        for (uint32_t x = w; x; x &= x - 1) {
-            const int k = __builtin_ctz(x);
-            if (owner[tid * 32 + k] != INT32_MAX) w &= ~(1u << k);
+    if (!fits) {                         // the new rows one by one
+        for (int s = part + a.parts * (tid >> 6); s < a.S_to; s += a.parts * (MT / 64)) {
+            int src, len, keep;
+            fork_head(a, s, src, len, keep);
+            for (int j = tid & 63; j < keep >> a.c.log2p; j += 64) {
+                const uint32_t x = (uint32_t)a.table[(int64_t)src * a.ld_table + j] - (uint32_t)b0;
+                if (x < RB) atomicOr(&sm.whole[x >> 5], 1u << (x & 31));
+            }
         }
-        n = __popc(w);
-        if (b0 + tid * 32 < a.c.n_blocks) a.freed[blockIdx.x * RW + tid] = w;
     }
-    n = block_sum<MT>(n, red);
-    if (tid == 0) {
-        a.counts[blockIdx.x] = n;
-        if (first) *a.bad = bad;
+    if (bad) sm.bad = 1;
+    __syncthreads();
+    const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
+    if (tid < RW && word < words) {
+        a.old[part * words + word] = sm.old[tid];
+        a.whole[part * words + word] = sm.whole[tid];
     }
+    if (first && tid == 0) a.bad[part] = sm.bad;
+}
+
+// the parts together: which blocks of the range are freed, and which sequences take a fresh block for one of it
+DD_DEV void fork_join(const ForkArgs& a, ForkLds& sm, int range) {
+    const int tid = threadIdx.x, b0 = range * RB;
+    const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
+    for (int i = tid; i < RB; i += MT) sm.owner[i] = INT32_MAX;
+    if (tid < RW) {
+        uint32_t old = 0, whole = 0;
+#pragma unroll 8
+        for (int k = 0; k < a.parts; ++k) {
+            old |= word < words ? a.old[k * words + word] : 0;
+            whole |= word < words ? a.whole[k * words + word] : 0;
+        }
+        sm.old[tid] = old;
+        sm.whole[tid] = whole;
+        sm.last[tid] = 0;
+    }
+    const bool bad = __syncthreads_or(tid < a.parts && a.bad[tid]);
+    int mine = -1;                       // this thread's first sequence's partly filled last block
     for (int s = tid; s < a.S_to; s += MT) {
-        int src, len, keep, b = -1;
+        int src, len, keep;
         fork_head(a, s, src, len, keep);
-        const bool part = len > 0 && (keep & (a.c.P - 1));
-        if (part) b = a.table[(int64_t)src * a.ld_table + len - 1];
+        if (!(keep & (a.c.P - 1))) {
+            if (range == 0) a.copies[s] = 0;
+            continue;
+        }
+        const int b = a.table[(int64_t)src * a.ld_table + len - 1];
         const uint32_t x = (uint32_t)b - (uint32_t)b0;
-        if (part && x < RB) a.copies[s] = owner[x] != s;
-        if (first && (!part || b < 0 || b >= a.c.n_blocks)) a.copies[s] = 0;
+        if (range == 0 && (uint32_t)b >= (uint32_t)a.c.n_blocks) a.copies[s] = 0;
+        if (x >= RB) continue;
+        if (s == tid) mine = b;
+        atomicMin(&sm.owner[x], s);
+        atomicOr(&sm.last[x >> 5], 1u << (x & 31));
     }
+    __syncthreads();
+    for (int s = tid; s < a.S_to; s += MT) {
+        int b = mine;
+        if (s != tid) {
+            int src, len, keep;
+            fork_head(a, s, src, len, keep);
+            b = keep & (a.c.P - 1) ? a.table[(int64_t)src * a.ld_table + len - 1] : -1;
+        }
+        const uint32_t x = (uint32_t)b - (uint32_t)b0;
+        if (x < RB && b < a.c.n_blocks) a.copies[s] = (sm.whole[x >> 5] >> (x & 31) & 1) || sm.owner[x] != s;
+    }
+    uint32_t w = tid < RW ? sm.old[tid] & ~sm.whole[tid] & ~sm.last[tid] : 0;
+    if (tid < RW && word < words) a.freed[word] = w;
+    const int n = block_sum<MT>(__popc(w), sm.red);
+    if (tid == 0) a.counts[range] = n;
+    if (range == 0 && tid == 0) a.bad[0] = bad;
 }
 
 // the r-th freed block in ascending order, by a wavefront
@@ -203,159 +260,246 @@ DD_DEV int nth_freed(const ForkArgs& a, int r) {
     }
 }
 
-__global__ __launch_bounds__(AT) void fork_apply_kernel(ForkArgs a) {
-    __shared__ int red[AT / 64];
-    constexpr int W = AT / 64;
+// NT threads; workgroup wg of `wgs`
+template <int NT>
+DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
+    constexpr int W = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int s0 = blockIdx.x * W;                 // sequences of this workgroup, one per wavefront
+    const int s0 = wg * W;                         // sequences of this workgroup, one per wavefront
     const int32_t n_free = *a.n_free;
+    const int bad = a.bad[0];
     int before = 0, all = 0, freed = 0;
-    for (int s = tid; s < a.S_to; s += AT) {
+    for (int s = tid; s < a.S_to; s += NT) {
         const int c = a.copies[s];
         all += c;
         before += s < s0 ? c : 0;
     }
-    for (int t = tid; t < a.ranges; t += AT) freed += a.counts[t];
-    all = block_sum<AT>(all, red);
-    before = block_sum<AT>(before, red);
-    freed = block_sum<AT>(freed, red);
-    const bool ok = !*a.bad && n_free >= 0 && n_free <= a.c.n_blocks && (int64_t)n_free + freed <= a.c.n_blocks &&
+    for (int t = tid; t < a.ranges; t += NT) freed += a.counts[t];
+    all = block_sum<NT>(all, red);
+    before = block_sum<NT>(before, red);
+    freed = block_sum<NT>(freed, red);
+    const bool ok = !bad && n_free >= 0 && n_free <= a.c.n_blocks && (int64_t)n_free + freed <= a.c.n_blocks &&
                     all <= (int64_t)n_free + freed;
-    if (blockIdx.x == 0 && tid == 0) {
+    if (wg == 0 && tid == 0) {
         if (!ok && a.err) atomicOr(a.err, DD_DEVERR_CACHE);
         *a.n_free_out = ok ? n_free + freed - all : n_free;
         *a.n_moves = ok ? all : 0;
     }
-    const int s = s0 + wv;
-    if (s < a.S_to) {
-        int src = 0, len = 0, keep = 0;
-        if (ok) fork_head(a, s, src, len, keep);
-        if (lane == 0) {
-            a.to_held[s] = len;
-            a.to_len[s] = keep;
-        }
-        const int32_t* from = a.table + (int64_t)src * a.ld_table;
-        int32_t* to = a.to_table + (int64_t)s * a.ld_to;
-        const bool copy = ok && a.copies[s];
-        for (int j = lane; j < len - copy; j += 64) to[j] = from[j];
-        if (copy) {
-            int rank = before;
-            for (int i = 0; i < wv; ++i) rank += a.copies[s0 + i];
-            // the top of the stack once the freed blocks are on it
-            const int at = n_free + freed - 1 - rank;
-            const int b = at < n_free ? a.free_blocks[at] : nth_freed(a, at - n_free);
+    for (int s1 = s0; s1 < a.S_to; s1 += wgs * W) {      // (one pass where there are as many workgroups as that)
+        const int s = s1 + wv;
+        if (s < a.S_to) {
+            int src = 0, len = 0, keep = 0;
+            if (ok) fork_head(a, s, src, len, keep);
             if (lane == 0) {
-                to[len - 1] = b;
-                a.moves[2 * rank] = from[len - 1];
-                a.moves[2 * rank + 1] = b;
-                if ((b < 0 || b >= a.c.n_blocks) && a.err) atomicOr(a.err, DD_DEVERR_CACHE);
+                a.to_held[s] = len;
+                a.to_len[s] = keep;
             }
+            const int32_t* from = a.table + (int64_t)src * a.ld_table;
+            int32_t* to = a.to_table + (int64_t)s * a.ld_to;
+            const bool copy = ok && a.copies[s];
+            for (int j = lane; j < len - copy; j += 64) to[j] = from[j];
+            if (copy) {
+                int rank = before;
+                for (int i = s1; i < s; ++i) rank += a.copies[i];
+                // the top of the stack once the freed blocks are on it
+                const int at = n_free + freed - 1 - rank;
+                const int b = at < n_free ? a.free_blocks[at] : nth_freed(a, at - n_free);
+                if (lane == 0) {
+                    to[len - 1] = b;
+                    a.moves[2 * rank] = from[len - 1];
+                    a.moves[2 * rank + 1] = b;
+                    if ((b < 0 || b >= a.c.n_blocks) && a.err) atomicOr(a.err, DD_DEVERR_CACHE);
+                }
+            }
+        }
+        if (s1 + wgs * W < a.S_to) {
+            int c = 0;
+            for (int i = s1 + tid; i < min(s1 + wgs * W, a.S_to); i += NT) c += a.copies[i];
+            before += block_sum<NT>(c, red);
         }
     }
     if (!ok) return;
     // the freed blocks of a range, one word per thread
     int base = n_free, done = 0;
-    for (int t = blockIdx.x; t < a.ranges; t += gridDim.x) {
+    for (int t = wg; t < a.ranges; t += wgs) {
         int sum = 0;
-        for (int x = done + tid; x < t; x += AT) sum += a.counts[x];
-        base += block_sum<AT>(sum, red);
+        for (int x = done + tid; x < t; x += NT) sum += a.counts[x];
+        base += block_sum<NT>(sum, red);
         done = t;
         const int64_t word = (int64_t)t * RW + tid;
-        uint32_t x = word * 32 < a.c.n_blocks ? a.freed[word] : 0;
-        int i = base + block_before<AT>(__popc(x), red);
+        uint32_t x = tid < RW && word * 32 < a.c.n_blocks ? a.freed[word] : 0;
+        int i = base + block_before<NT>(__popc(x), red);
         for (; x; x &= x - 1) a.free_blocks[i++] = (int32_t)(word * 32) + __builtin_ctz(x);
     }
 }
 
+__global__ __launch_bounds__(MT) void fork_mark_kernel(ForkArgs a) {
+    __shared__ ForkLds sm;
+    fork_mark(a, sm, blockIdx.x, blockIdx.y);
+}
+__global__ __launch_bounds__(MT) void fork_join_kernel(ForkArgs a) {
+    __shared__ ForkLds sm;
+    fork_join(a, sm, blockIdx.x);
+}
+__global__ __launch_bounds__(AT) void fork_apply_kernel(ForkArgs a) {
+    __shared__ int red[AT / 64];
+    fork_apply<AT>(a, red, blockIdx.x, gridDim.x);
+}
+// all of it for a pool of one range and few sequences: one launch
+__global__ __launch_bounds__(MT) void fork_kernel(ForkArgs a) {
+    __shared__ ForkLds sm;
+    fork_mark(a, sm, 0, 0);
+    __threadfence_block();
+    __syncthreads();
+    fork_join(a, sm, 0);
+    __threadfence_block();
+    __syncthreads();
+    fork_apply<MT>(a, sm.red, 0, 1);
+}
+
 // ---------------------------------------------------------------- compaction
 //
-// n blocks are in use.  The i-th used block >= n moves to the i-th number below n that is not used.
-__global__ __launch_bounds__(MT) void compact_mark_kernel(CompactArgs a) {
-    __shared__ uint32_t used[RW];
-    __shared__ int red[MT / 64], bad;
-    const int tid = threadIdx.x, b0 = blockIdx.x * RB;
-    if (tid < RW) used[tid] = 0;
-    if (tid == 0) bad = 0;
+// n blocks are in use.  The i-th used block >= n moves to the i-th number below n that is not used.  With used(b) blocks in use below
+// b, block b >= n is number used(b) - used(n) of those that move, and an unused number h < n is number h - used(h) of those
+// that they move to: each writes its half of a move, and the tables look theirs up.
+struct CompactLds {
+    uint32_t used[RW];
+    int32_t start[PAGE_RANGES];         // used blocks before each range
+    int red[MT / 64], bad;
+};
+
+DD_DEV void compact_mark(const CompactArgs& a, CompactLds& sm, int range, int part) {
+    const int tid = threadIdx.x, b0 = range * RB;
+    if (tid < RW) sm.used[tid] = 0;
+    if (tid == 0) sm.bad = 0;
     __syncthreads();
-    walk<MT>(a.table, a.ld_table, a.S,
-             [&](int q, int& src, int& len) {
-                 src = q;
-                 if (!held_ok(a.held, a.ld_table, q, len)) bad = 1;
+    bool bad = false;
+    walk<MT>(a.table, a.ld_table, a.S, part, a.parts,
+             [&](int q) {
+                 int len;
+                 bad |= !held_ok(a.held, a.ld_table, q, len);
+                 return Head{len, 0};
              },
-             [&](int b, int, int, int) {
-                 if (b < 0 || b >= a.c.n_blocks) bad = 1;
+             [&](int b, int j, const Head& h) {
+                 if (range == 0) bad |= wrong(b, j, h, a.c.n_blocks);
                  const uint32_t x = (uint32_t)b - (uint32_t)b0;
-                 if (x < RB) atomicOr(&used[x >> 5], 1u << (x & 31));
+                 if (x < RB) atomicOr(&sm.used[x >> 5], 1u << (x & 31));
              });
+    if (bad) sm.bad = 1;
     __syncthreads();
-    const int c = tid < RW ? __popc(used[tid]) : 0;
-    const int before = block_before<MT>(c, red);
-    if (tid < RW && b0 + tid * 32 < a.c.n_blocks) {
-        a.used[blockIdx.x * RW + tid] = used[tid];
-        a.before[blockIdx.x * RW + tid] = before;
+    const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
+    if (tid < RW && word < words) a.used[part * words + word] = sm.used[tid];
+    if (range == 0 && tid == 0) a.bad[part] = sm.bad;
+}
+
+// the parts together, into the first one's bits
+DD_DEV void compact_join(const CompactArgs& a, CompactLds& sm, int range) {
+    const int tid = threadIdx.x;
+    const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
+    uint32_t x = 0;
+    if (tid < RW && word < words)
+#pragma unroll 8
+        for (int k = 0; k < a.parts; ++k) x |= a.used[k * words + word];
+    const bool bad = __syncthreads_or(tid < a.parts && a.bad[tid]);
+    const int before = block_before<MT>(__popc(x), sm.red);
+    if (tid < RW && word < words) {
+        a.used[word] = x;
+        a.before[word] = before;
     }
-    if (tid == RW - 1) {
-        a.counts[blockIdx.x] = before + c;
-        if (blockIdx.x == 0) *a.bad = bad;
+    if (tid == RW - 1) a.counts[range] = before + __popc(x);
+    if (range == 0 && tid == 0) a.bad[0] = bad;
+}
+
+// used blocks before each range into start; their number
+template <int NT>
+DD_DEV int compact_starts(const CompactArgs& a, int32_t* start, int* red) {
+    int n = 0;
+    for (int t0 = 0; t0 < a.ranges; t0 += NT) {
+        const int t = t0 + threadIdx.x, c = t < a.ranges ? a.counts[t] : 0;
+        const int before = n + block_before<NT>(c, red);
+        if (t < a.ranges) start[t] = before;
+        n += block_sum<NT>(c, red);
+    }
+    __syncthreads();
+    return n;
+}
+DD_DEV int used_before(const CompactArgs& a, const int32_t* start, int b) {      // b below n_blocks
+    return start[b / RB] + a.before[b >> 5] + __popc(a.used[b >> 5] & ((1u << (b & 31)) - 1u));
+}
+
+// the moves and the stack
+template <int NT>
+DD_DEV void compact_moves(const CompactArgs& a, const int32_t* start, int n, int wg, int wgs) {
+    const int nb = a.c.n_blocks;
+    const int low = n < nb ? used_before(a, start, n) : n;     // used blocks below n: they stay
+    const bool ok = !a.bad[0];
+    if (wg == 0 && threadIdx.x == 0) {
+        *a.n_moves = ok ? n - low : 0;
+        if (ok) *a.n_free_out = nb - n;
+        else if (a.err) atomicOr(a.err, DD_DEVERR_CACHE);
+    }
+    if (!ok) return;
+    for (int64_t i = (int64_t)wg * NT + threadIdx.x; i < nb; i += (int64_t)wgs * NT) {
+        const int b = (int)i;
+        if (i < nb - n) a.free_blocks[i] = nb - 1 - b;
+        const bool in = a.used[b >> 5] >> (b & 31) & 1;
+        if (in == (b < n)) continue;
+        const int u = used_before(a, start, b);
+        if (in) a.moves[2 * (u - low)] = b;
+        else a.moves[2 * (b - u) + 1] = b;
     }
 }
 
-__global__ __launch_bounds__(AT) void compact_apply_kernel(CompactArgs a) {
-    __shared__ int32_t start[PAGE_RANGES];         // used blocks before each range
-    __shared__ int red[AT / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    int n = 0;
-    for (int t0 = 0; t0 < a.ranges; t0 += AT) {
-        const int c = t0 + tid < a.ranges ? a.counts[t0 + tid] : 0;
-        const int before = n + block_before<AT>(c, red);
-        if (t0 + tid < a.ranges) start[t0 + tid] = before;
-        n += block_sum<AT>(c, red);
-    }
-    __syncthreads();
-    const int nb = a.c.n_blocks;
-    const bool ok = !*a.bad;
-    auto used_before = [&](int b) {                // used blocks below b < nb
-        return start[b / RB] + a.before[b >> 5] + __popc(a.used[b >> 5] & ((1u << (b & 31)) - 1u));
-    };
-    const int low = n < nb ? used_before(n) : n;   // used blocks below n: they stay
-    auto hole = [&](int r) {                       // the r-th number below n that is not used
-        int lo = 0, hi = (n - 1) >> 5;             // the last word that fewer or as many as r free numbers stand before
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (mid * 32 - (start[mid / RW] + a.before[mid]) <= r) lo = mid;
-            else hi = mid - 1;
-        }
-        return lo * 32 + nth_bit(~a.used[lo], r - (lo * 32 - (start[lo / RW] + a.before[lo])));
-    };
-    const int gw = blockIdx.x * (AT / 64) + wv, waves = gridDim.x * (AT / 64);
-    for (int q = gw; q < a.S; q += waves) {
+// the tables under the new numbers
+template <int NT>
+DD_DEV void compact_tables(const CompactArgs& a, const int32_t* start, int n, int wg, int wgs) {
+    const int lane = threadIdx.x & 63, nb = a.c.n_blocks;
+    const int low = n < nb ? used_before(a, start, n) : n;
+    const bool ok = !a.bad[0];
+    for (int q = wg * (NT / 64) + (threadIdx.x >> 6); q < a.S; q += wgs * (NT / 64)) {
         int len;
         held_ok(a.held, a.ld_table, q, len);
         const int32_t* from = a.table + (int64_t)q * a.ld_table;
         int32_t* to = a.to_table + (int64_t)q * a.ld_table;
         for (int j = lane; j < len; j += 64) {
             const int b = from[j];
-            to[j] = ok && b >= n ? hole(used_before(b) - low) : b;
+            to[j] = ok && b >= n ? a.moves[2 * (used_before(a, start, b) - low) + 1] : b;
         }
     }
-    if (blockIdx.x == 0 && tid == 0) {
-        if (ok) {
-            *a.n_free_out = nb - n;
-            *a.n_moves = n - low;
-        } else {
-            *a.n_moves = 0;
-            if (a.err) atomicOr(a.err, DD_DEVERR_CACHE);
-        }
-    }
-    if (!ok) return;
-    const int64_t step = (int64_t)gridDim.x * AT, at = (int64_t)blockIdx.x * AT + tid;
-    for (int64_t i = at; i < nb - n; i += step) a.free_blocks[i] = (int32_t)(nb - 1 - i);
-    for (int64_t b = n + at; b < nb; b += step)
-        if (a.used[b >> 5] >> (b & 31) & 1) {
-            const int r = used_before((int)b) - low;
-            a.moves[2 * r] = (int32_t)b;
-            a.moves[2 * r + 1] = hole(r);
-        }
+}
+
+__global__ __launch_bounds__(MT) void compact_mark_kernel(CompactArgs a) {
+    __shared__ CompactLds sm;
+    compact_mark(a, sm, blockIdx.x, blockIdx.y);
+}
+__global__ __launch_bounds__(MT) void compact_join_kernel(CompactArgs a) {
+    __shared__ CompactLds sm;
+    compact_join(a, sm, blockIdx.x);
+}
+__global__ __launch_bounds__(AT) void compact_moves_kernel(CompactArgs a) {
+    __shared__ int32_t start[PAGE_RANGES];
+    __shared__ int red[AT / 64];
+    compact_moves<AT>(a, start, compact_starts<AT>(a, start, red), blockIdx.x, gridDim.x);
+}
+__global__ __launch_bounds__(AT) void compact_tables_kernel(CompactArgs a) {
+    __shared__ int32_t start[PAGE_RANGES];
+    __shared__ int red[AT / 64];
+    compact_tables<AT>(a, start, compact_starts<AT>(a, start, red), blockIdx.x, gridDim.x);
+}
+// all of it for a pool of one range and few sequences: one launch
+__global__ __launch_bounds__(MT) void compact_kernel(CompactArgs a) {
+    __shared__ CompactLds sm;
+    compact_mark(a, sm, 0, 0);
+    __threadfence_block();
+    __syncthreads();
+    compact_join(a, sm, 0);
+    __threadfence_block();
+    __syncthreads();
+    const int n = compact_starts<MT>(a, sm.start, sm.red);
+    compact_moves<MT>(a, sm.start, n, 0, 1);
+    __threadfence_block();
+    __syncthreads();
+    compact_tables<MT>(a, sm.start, n, 0, 1);
 }
 
 // ---------------------------------------------------------------- copy
@@ -398,24 +542,46 @@ __global__ __launch_bounds__(CT) void copy_kernel(CopyArgs a) {
 
 }  // namespace
 
-dd_status launch_cache_fork(const ForkArgs& a, hipStream_t s) {
-    {
+// Sequences up to which one workgroup does everything for a pool of one range (16 sequences compact in 7 us, and took 9 in three
+// launches); sequences of a part, two for a wavefront.
+constexpr int ONE_LAUNCH = 128, PER_PART = 2 * MT / 64;
+
+static int parts_for(int ranges, int32_t S) { return std::max(1, std::min(page_parts(ranges), S / PER_PART)); }
+
+dd_status launch_cache_fork(const ForkArgs& args, hipStream_t s) {
+    ForkArgs a = args;
+    auto go = [&](auto kernel, dim3 grid, int threads) {
         ProfScope ps(KC_CACHE_FORK, s);
-        launch_k(fork_mark_kernel, dim3((unsigned)a.ranges), dim3(MT), 0, s, a);
+        launch_k(kernel, grid, dim3(threads), 0, s, a);
+    };
+    if (a.ranges == 1 && a.S <= ONE_LAUNCH && a.S_to <= ONE_LAUNCH) {
+        a.parts = 1;
+        go(fork_kernel, dim3(1), MT);
+        return launch_status("cache_fork");
     }
-    ProfScope ps(KC_CACHE_FORK, s);
-    launch_k(fork_apply_kernel, dim3((unsigned)std::max<int64_t>(1, ceil_div(a.S_to, AT / 64))), dim3(AT), 0, s, a);
+    a.parts = parts_for(a.ranges, a.S);
+    go(fork_mark_kernel, dim3((unsigned)a.ranges, (unsigned)a.parts), MT);
+    go(fork_join_kernel, dim3((unsigned)a.ranges), MT);
+    go(fork_apply_kernel, dim3((unsigned)std::max<int64_t>(1, ceil_div(a.S_to, AT / 64))), AT);
     return launch_status("cache_fork");
 }
 
-dd_status launch_cache_compact(const CompactArgs& a, hipStream_t s) {
-    {
+dd_status launch_cache_compact(const CompactArgs& args, hipStream_t s) {
+    CompactArgs a = args;
+    auto go = [&](auto kernel, dim3 grid, int threads) {
         ProfScope ps(KC_CACHE_COMPACT, s);
-        launch_k(compact_mark_kernel, dim3((unsigned)a.ranges), dim3(MT), 0, s, a);
+        launch_k(kernel, grid, dim3(threads), 0, s, a);
+    };
+    if (a.ranges == 1 && a.S <= ONE_LAUNCH) {
+        a.parts = 1;
+        go(compact_kernel, dim3(1), MT);
+        return launch_status("cache_compact");
     }
-    ProfScope ps(KC_CACHE_COMPACT, s);
-    const int64_t wgs = std::max(ceil_div(a.S, AT / 64), ceil_div(a.c.n_blocks, 4 * AT));
-    launch_k(compact_apply_kernel, dim3((unsigned)std::min<int64_t>(1024, wgs)), dim3(AT), 0, s, a);
+    a.parts = parts_for(a.ranges, a.S);
+    go(compact_mark_kernel, dim3((unsigned)a.ranges, (unsigned)a.parts), MT);
+    go(compact_join_kernel, dim3((unsigned)a.ranges), MT);
+    go(compact_moves_kernel, dim3((unsigned)std::min<int64_t>(1024, ceil_div(a.c.n_blocks, AT))), AT);
+    go(compact_tables_kernel, dim3((unsigned)std::min<int64_t>(1024, std::max<int64_t>(1, ceil_div(a.S, AT / 64)))), AT);
     return launch_status("cache_compact");
 }
 
