@@ -505,9 +505,12 @@ __global__ __launch_bounds__(MT) void compact_kernel(CompactArgs a) {
 // ---------------------------------------------------------------- copy
 //
 // A block's codes of all heads stand one behind the other, H 2 P dh bytes, and so do its scales.  A workgroup copies a piece of
-// one block in one layer.
-constexpr int CT = 256, CL = 4;           // threads, 16-byte loads of each
-constexpr int PIECE = CT * CL * 16;
+// one block in one layer, 16 bytes per thread, and takes another while there are any: how many moves there are, only the
+// device knows.  Bound by the memory: 4.9 TB/s read and written at 1024 moves of 98304 bytes in 12 layers, 492 us; 16 of them
+// take 7.7.  One load per thread and many short workgroups: two or four loads per thread cost the small copy 9 us, and the large
+// one 5.  16 workgroups per CU and not as many as there are pieces: 484 us at 64 per CU, but an empty list would pay for those.
+constexpr int CT = 512;
+constexpr int PIECE = CT * 16;
 
 __global__ __launch_bounds__(CT) void copy_kernel(CopyArgs a) {
     const int tid = threadIdx.x;
@@ -525,13 +528,7 @@ __global__ __launch_bounds__(CT) void copy_kernel(CopyArgs a) {
         const uint8_t* src = a.codes + (lay + from) * a.slab;
         uint8_t* dst = a.codes + (lay + to) * a.slab;
         const int64_t at = (int64_t)piece * PIECE + tid * 16;
-        uint4 u[CL];
-#pragma unroll
-        for (int k = 0; k < CL; ++k)
-            if (at + k * CT * 16 < a.slab) u[k] = *(const uint4*)(src + at + k * CT * 16);
-#pragma unroll
-        for (int k = 0; k < CL; ++k)
-            if (at + k * CT * 16 < a.slab) *(uint4*)(dst + at + k * CT * 16) = u[k];
+        if (at < a.slab) *(uint4*)(dst + at) = *(const uint4*)(src + at);
         if (piece == 0) {
             const float2* ss = (const float2*)a.scales + (lay + from) * a.heads;
             float2* sd = (float2*)a.scales + (lay + to) * a.heads;
@@ -588,7 +585,7 @@ dd_status launch_cache_compact(const CompactArgs& args, hipStream_t s) {
 dd_status launch_cache_copy(const CopyArgs& a, hipStream_t s) {
     const double units = (double)ceil_div(a.slab, PIECE) * a.max_moves * a.layers;
     ProfScope ps(KC_CACHE_COPY, s);
-    launch_k(copy_kernel, dim3((unsigned)std::min<double>(units, 8 * num_cus())), dim3(CT), 0, s, a);
+    launch_k(copy_kernel, dim3((unsigned)std::min<double>(units, 16 * num_cus())), dim3(CT), 0, s, a);
     return launch_status("cache_copy");
 }
 
