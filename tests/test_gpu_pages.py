@@ -70,7 +70,8 @@ class Pages:
 FORK = [  # sequences, new ones, blocks, P, entries per row of both tables
     (1, 1, 1, 32, 1, 1), (1, 16, 40, 64, 16, 16), (5, 5, 60, 32, 9, 9), (3, 40, 300, 128, 70, 70), (64, 64, 700, 64, 8, 8),
     (200, 150, 9000, 32, 30, 33), (65, 1, 16500, 256, 200, 190), (1000, 1024, 30000, 32, 25, 25), (7, 300, 8192, 64, 300, 300),
-    (4, 4, 8193, 64, 2000, 2000), (0, 3, 10, 32, 4, 4), (5, 0, 30, 32, 4, 4)]
+    (4, 4, 8193, 64, 2000, 2000), (0, 3, 10, 32, 4, 4), (5, 0, 30, 32, 4, 4),
+    (128, 128, 3000, 32, 8, 8), (129, 100, 3000, 64, 8, 8), (100, 129, 3000, 64, 8, 8), (8193, 300, 20000, 32, 3, 3), (600, 8200, 9000, 32, 3, 5)]
 
 
 @pytest.mark.parametrize("S,to,nb,P,ld,ld_to", FORK)
@@ -142,7 +143,8 @@ def test_a_stack_with_a_wrong_number():
         assert int(p.err.item()) == dd.DD_DEVERR_CACHE and p.to.block_table.tolist() == [[2, 3], [2, wrong]] and int(p.n_out.item()) == 1
 
 
-COMPACT = [(1, 1, 32, 1), (5, 60, 32, 9), (64, 2000, 64, 8), (300, 9000, 32, 30), (2, 8192, 64, 100), (1000, 40000, 32, 20), (4, 30, 32, 6), (0, 40, 32, 3)]
+COMPACT = [(1, 1, 32, 1), (5, 60, 32, 9), (64, 2000, 64, 8), (300, 9000, 32, 30), (2, 8192, 64, 100), (1000, 40000, 32, 20), (4, 30, 32, 6), (0, 40, 32, 3), (128, 8000, 32, 9),
+           (129, 8000, 32, 9), (4000, 30000, 32, 6)]
 
 
 @pytest.mark.parametrize("S,nb,P,ld", COMPACT)
@@ -226,6 +228,31 @@ def test_copies(layers, heads, dh, P, nb, n):
         dd.cache_copy(cc, c, s, dev_i32(torch, mv), dev_i32(torch, [count]), layers=layers, dev_err=err)
         assert torch.equal(c, wc) and torch.equal(s, wsc), count
         assert (int(err.item()) == dd.DD_DEVERR_CACHE) == (bad is not None and (count > n or count > 0))
+
+
+def test_a_pool_of_many_ranges():
+    """More ranges than CUs: as few parts as one."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(2)
+    S, nb, P, ld = 90, 2_200_000, 32, 40
+    c = pool(rng, S, nb, P, ld)
+    cc = dd.cache_config(nb, P, 1, 32)
+    src = rng.integers(0, S, 70)
+    p = Pages(torch, cc, 70, ld)
+    p.fork(c, src, None)
+    p.same(so.fork(nb, P, c[0], c[1], c[2], src, None, c[3], c[4], ld), c)
+    w = so.compact(nb, c[0], c[1])
+    m = dd.CacheMap.empty(S, 1, ld)
+    m.block_table.copy_(dev_i32(torch, c[0]))
+    m.held.copy_(dev_i32(torch, c[1]))
+    f, n_out, n_moves, moves = dev_i32(torch, np.zeros(nb)), dev_i32(torch, [0]), dev_i32(torch, [0]), dev_i32(torch, np.zeros((nb // 2, 2)))
+    dd.cache_compact(cc, m, m.block_table, f, n_out, moves, n_moves, torch.full((dd.cache_compact_workspace_bytes(cc),), 255, dtype=torch.uint8,
+                                                                                 device="cuda"))
+    n = len(w["moves"])
+    assert int(n_moves.item()) == n and [tuple(x) for x in moves[:n].tolist()] == w["moves"]
+    assert f[:int(n_out.item())].tolist() == w["free"]
+    got = m.block_table.cpu().numpy()
+    assert all(got[s, :c[1][s]].tolist() == w["rows"][s] for s in range(S))
 
 
 def test_copies_past_32_bits():

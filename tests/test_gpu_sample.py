@@ -283,3 +283,82 @@ def test_truncated_rows_in_the_draws_that_follow():
     dd.spec_verify(q, qd, "bf16", ld, S, B, V, draft, n_out, z_out, ws, seed=9, dev_err=err)
     last = q.view(S, B, ld)[:, B - 1]
     assert int(err.item()) == 0 and (n_out == B).all() and last.gather(1, z_out.long()[:, None]).isfinite().all()
+
+
+@pytest.mark.parametrize("V,dtype", [(v, "bf16") for v in (2048, 2049, 8192, 16384, 16385, 32768, 32769, 53248, 53249, 57344, 57345, 65536, 131072, 131073)] +
+                         [(4096, "fp32"), (4097, "fp32")])
+def test_sizes_at_which_another_kernel_begins(V, dtype):
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    R = 5
+    l = round_to_dtype(rng.normal(size=(R, V)) * np.array([0.2, 1.0, 3.0, 8.0, 3.0])[:, None], dtype)
+    l[4, rng.random(V) < 0.5] = -np.inf
+    l[:, 0], l[:, V - 1] = 3.0, 3.5
+    check(torch, l, dtype, [dict(OFF, top_p=0.8), dict(OFF, top_k=V // 3, temperature=1.5), dict(OFF, top_k=40, top_p=0.9),
+                            dict(OFF, min_p=0.001), dict(OFF)], words_of(rng, R), sure=0.6)
+
+
+@pytest.mark.parametrize("V,dtype", [(1500, "bf16"), (50257, "bf16"), (55000, "bf16"), (140000, "bf16"), (3000, "fp32"), (20000, "fp32")])
+def test_many_rows_equal_few(V, dtype):
+    """A call of more rows than CUs equals calls of some of them, bit for bit: sums do not depend on the kernel."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    R, part, ld = 2 * torch.cuda.get_device_properties(0).multi_processor_count + 77, 97, int(dd.logits_ld(V))
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((R, ld), generator=g, device="cuda") * torch.rand((R, 1), generator=g, device="cuda") * 6
+    x[torch.rand((R, ld), generator=g, device="cuda") < 0.05] = -np.inf
+    x[:, V // 2] = 1.0
+    x = x.bfloat16() if dtype == "bf16" else x
+    s, words = draw_settings(rng, R, V), words_of(rng, R)
+    got = []
+    for step in (R, part):
+        z, n, n2, err = (dev_i32(torch, np.full(k, -9)) for k in (R, R, R, 1))
+        err.zero_()
+        logp, out = torch.zeros(R, device="cuda"), torch.full_like(x, 3.0)
+        for i in range(0, R, step):
+            j = min(R, i + step)
+            a = settings(torch, s[i:j], NAMES)
+            dd.token_sample(x[i:j], dtype, ld, j - i, V, z[i:j], j - i, noise_words=dev_words(torch, words[i:j]), logp=logp[i:j], n_kept=n[i:j],
+                            dev_err=err, **a)
+            dd.logits_truncate(x[i:j], dtype, ld, j - i, V, out[i:j], n_kept=n2[i:j], dev_err=err, **a)
+        assert int(err.item()) == 0 and torch.equal(n, n2)
+        got.append((z, n, logp, out))
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("V,dtype", [(3000, "fp32"), (9000, "fp32"), (132000, "bf16")])
+def test_draws_of_one_row_equal_single_ones(V, dtype):
+    """Runs of draws from one row, also across rows left out, numbers out of range, rows that allow nothing, greedy draws and
+    settings of which some do not hold, equal the same draws in calls of few."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    R, per, ld = 12, 7, int(dd.logits_ld(V))
+    n = 7 * cus + 5
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((R, ld), generator=g, device="cuda") * 3
+    x[3, 5], x[4] = np.nan, -np.inf
+    x = x.bfloat16() if dtype == "bf16" else x
+    ids = np.repeat(rng.integers(0, R, n // 50 + 1), 50)[:n]
+    ids[rng.random(n) < 0.05] = -1
+    ids[[40, 41, 300]] = [R, -2, 2 ** 31 - 1]
+    S = -(-n // per)
+    s = draw_settings(rng, S, V)
+    s[9]["temperature"], s[20]["top_p"], s[21]["min_p"] = -1.0, -0.5, 2.0
+    words = words_of(rng, n)
+    got = []
+    step = per * (cus // per)
+    for most in (n, step):
+        z, kept, err = dev_i32(torch, np.full(n, -9)), dev_i32(torch, np.full(n, -9)), dev_i32(torch, [0])
+        logp = torch.full((n,), 7.0, device="cuda")
+        for i in range(0, n, most):
+            j = min(n, i + most)
+            dd.token_sample(x, dtype, ld, R, V, z[i:j], j - i, row_ids=dev_i32(torch, ids[i:j]), draws_per_seq=per,
+                            noise_words=dev_words(torch, words[i:j]), logp=logp[i:j], n_kept=kept[i:j], dev_err=err,
+                            **settings(torch, s[i // per:-(-j // per)], NAMES))
+        assert int(err.item()) == dd.DD_DEVERR_SAMPLING | dd.DD_DEVERR_LOGITS
+        got.append((z, kept, torch.nan_to_num(logp, nan=-77.0)))
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
+    assert (got[0][0][dev_i32(torch, ids) == -1] == -9).all() and len(set(got[0][0].tolist())) > 100
