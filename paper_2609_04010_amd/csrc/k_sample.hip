@@ -3,12 +3,16 @@
 // Classes in order: falling logit l, the lowest index first among equal ones; w = exp((l - max) / temperature).  What
 // stays is a beginning of that order (min-p cuts it at a value, top-k at a count, top-p at a sum of weights), and the draw is
 // the first class at which the running sum exceeds u times the sum of what stays: every step but min-p asks for
-// the first class at which a running sum (of ones, or of weights) reaches a bound.  That is answered without sorting:
-// a histogram of counts and weights over NB bins of equal width in l, its prefix sums, the bin where the bound lies, and the
-// classes of that bin one by one (a bin of more than 64 is cut again by its numbers' bits and indices).
+// the first class at which a running sum (of ones, or of weights) reaches a bound.  That is answered without sorting: counts
+// and weights of a histogram's bins, in falling order of l, their prefix sums, the bin where the bound lies, and the
+// classes of that bin one by one.  bf16 rows of up to 131072 classes have a kernel of their own: their numbers are few.
 //
-// Sums of weights are whole numbers, multiples of 2^-46 (the exponential is taken in 64 bits and rounded once), so that neither the
-// order of the atomics nor the cut into bins shows, and no border moves by more than 2^-47 per class.
+// Sums of weights are whole numbers, multiples of 2^-46 (coarser where 2^16 classes of weight 1 would pass 62 bits; the
+// exponential is taken in 64 bits and rounded once), so that neither the order of the atomics nor the cut into bins shows, and
+// no border moves by more than half of that per class.
+//
+// A row is one workgroup's: its phases (largest number, histogram, sums, search) follow each other, so a call of few rows is
+// bound by latency, and one of many by the instructions of the histogram and the search, not by reading the row.
 #include <float.h>
 #include <math.h>
 
@@ -35,7 +39,7 @@ DD_DEV float key_value(uint32_t k) {
 DD_DEV uint64_t place(float l, int v) { return ((uint64_t)value_key(l) << 32) | (uint32_t)v; }
 
 constexpr int TAB = 64;      // 2^(-j / TAB)
-constexpr int EQUALS = 256;  // equal numbers that are
+constexpr int EQUALS = 256;  // equal numbers that are ordered one by one (more are counted)
 
 // what a row's weights are made of
 struct RowScale {
@@ -89,10 +93,13 @@ DD_DEV bool quotient_fits(float t, float a, float b) {
 //
 // A bf16 number's 16 bits, as a signed whole number that orders like it (k = +-magnitude), are a bin of their own: equal
 // numbers are all that a bin holds, so a count gives its weight, the exponential is taken once per bin, and a bound
-// inside a bin is a division away.  A window of keys stands in LDS: MAGS magnitudes of either sign below the largest that can matter (weights
-// below e^-34 round to 0), with the numbers nearer to 0 in one bin between them, whose weights are summed one by one (few:
+// inside a bin is a division away.  A window of keys stands in LDS: MAGS magnitudes of either sign below the largest that can
+// matter (weights below e^-34 round to 0), with the numbers nearer to 0 in one bin between them, whose weights are summed one by one (few:
 // the window spans 16 binades).  Where a bound falls among those, or among numbers below the window (top-k alone can ask for
-// them), the next window is counted.  Two packed numbers are handled at a time.
+// them), the next window is counted.  Two packed numbers are handled at a time, and the row stays in registers.
+//
+// Rows of 50257 classes under temperature, top-k and top-p: 8 in 16 us, 512 in 30; 4096 truncated in 174 (4.7 TB/s read and
+// written; with a division per number and its edges tested one by one 560).
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
@@ -728,10 +735,10 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
 // ---------------------------------------------------------------- fp32 rows, and bf16 rows of very many classes
 //
 // Every pass reads the row again, from L2 after the first.  (With the row in registers, 52 of them, the compiler keeps
-// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 65.)  Bins are steps of the exponential's table, so a
-// number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
+// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 65.)  Bins are steps of the exponential's
+// table, so a number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
 // of the bin where a bound lies are listed with their weights, and each sums those before it.  Draws that follow each
-// other from one row under the same settings share all but the last step.
+// other from one row under the same settings share all but the last step.  333 truncated rows of 32003 take 55 us.
 template <int NT>
 struct StreamLds {
     static constexpr int NW = NT / 64;
@@ -1236,12 +1243,19 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
 template <bool DRAW>
 static void launch_sample_keys(const SampleArgs& a, hipStream_t s) {
     auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)a.n), dim3(threads), 0, s, a); };
-    // A row's time is that of its phases one behind the other: with a CU for each row it ends sooner in 1024 threads; where
-    // rows wait for CUs, two of 512 threads on a CU do less work each.
-    const bool few = a.n <= num_cus();
+    // A CU holds 1024 such threads, in one workgroup or several: a row ends soonest in many threads, and many rows cost least in
+    // few each (a wavefront's share of the search is the same for any).  At up to a CU, up to two and more rows per CU, draws
+    // under top-p: 32000 classes, 200 rows 14.0 us in 1024 threads and 15.1 in 512, 300 rows 24.1 and 19.7; 8000 classes, 500 rows 13.8
+    // in 512 and 14.7 in 256, 700 rows 19.8 and 17.0; 16000 classes, 500 rows 16.2 and 17.7, 1024 rows 28.4 and 24.4;
+    // 50257 classes, 200 rows 17.9 in 1024 and 18.7 in 512, 300 rows 31.6 and 24.7.
+    const int cus = num_cus();
+    const bool few = a.n <= cus, some = a.n <= 2 * (int64_t)cus;
     if (a.V <= 2048) go(sample_keys_kernel<256, 1, DRAW>, 256);
+    else if (a.V <= 8192 && some) go(sample_keys_kernel<512, 2, DRAW>, 512);
     else if (a.V <= 8192) go(sample_keys_kernel<256, 4, DRAW>, 256);
-    else if (a.V <= 16384) go(sample_keys_kernel<512, 4, DRAW>, 512);
+    else if (a.V <= 16384 && some) go(sample_keys_kernel<512, 4, DRAW>, 512);
+    else if (a.V <= 16384) go(sample_keys_kernel<256, 8, DRAW>, 256);
+    else if (a.V <= 32768 && few) go(sample_keys_kernel<1024, 4, DRAW>, 1024);
     else if (a.V <= 32768) go(sample_keys_kernel<512, 8, DRAW>, 512);
     else if (a.V <= 57344 && few) go(sample_keys_kernel<1024, 7, DRAW>, 1024);
     else if (a.V <= 53248) go(sample_keys_kernel<512, 13, DRAW>, 512);
@@ -1256,11 +1270,15 @@ static void launch_sample_t(const SampleArgs& args, hipStream_t s) {
         if (a.V <= 131072 && grid_fits(a.n, 1024)) return launch_sample_keys<DRAW>(a, s);
     }
     // Draws that share a row and its settings are one workgroup's as far as every CU has one.
-    a.chunk = DRAW && a.per > 1 ? (int)std::max<int64_t>(1, a.n / num_cus()) : 1;
+    a.chunk = DRAW && a.per > 1 && a.row_ids ? (int)std::max<int64_t>(1, a.n / num_cus()) : 1;
     if (!grid_fits(ceil_div(a.n, a.chunk), 1024)) a.chunk = 1024;
     auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)ceil_div(a.n, a.chunk)), dim3(threads), 0, s, a); };
-    if (a.V <= 4096) return go(sample_stream_kernel<T, 256, DRAW>, 256);
-    if (ceil_div(a.n, a.chunk) > num_cus()) return go(sample_stream_kernel<T, 512, DRAW>, 512);
+    // As above: draws from 4000 classes, 200 rows 12.4 us in 256 threads and 13.3 in 512; from 16000, 300 rows 29.3 and 27.3, 700
+    // rows 38.3 and 42.4; from 32000, 200 rows 31.5 in 512 and 26.2 in 1024, 300 rows 42.3 and 48.9, 2048 rows 159.7 in 256 and 164.3
+    // in 512 (within the noise).
+    const int64_t groups = ceil_div(a.n, a.chunk), cus = num_cus();
+    if (a.V <= 4096 || (a.V <= 16384 && groups > 2 * cus)) return go(sample_stream_kernel<T, 256, DRAW>, 256);
+    if (groups > cus) return go(sample_stream_kernel<T, 512, DRAW>, 512);
     go(sample_stream_kernel<T, 1024, DRAW>, 1024);
 }
 

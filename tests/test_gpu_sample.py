@@ -205,6 +205,23 @@ def test_more_draws_than_workgroups():
     check(torch, l, "fp32", draw_settings(rng, R, V), words_of(rng, R), ld=ld)
 
 
+def test_more_draws_than_a_grid_holds():
+    """4.2 million rows of 5 classes equal their halves."""
+    torch = torch_or_skip()
+    V, ld, R = 5, 8, 2 ** 22 + 5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((R, ld), generator=g, device="cuda").bfloat16()
+    a, h = dict(seed=4), R // 2
+    z, z2, n, n2 = (torch.zeros(R, dtype=torch.int32, device="cuda") for _ in range(4))
+    p, out, out2 = torch.full((R,), 0.8, device="cuda"), torch.full_like(x, 3.0), torch.full_like(x, 3.0)
+    dd.token_sample(x, "bf16", ld, R, V, z, R, top_p=p, n_kept=n, **a)
+    dd.logits_truncate(x, "bf16", ld, R, V, out, top_p=p)
+    for i, k in ((0, h), (h, R - h)):
+        dd.token_sample(x[i:], "bf16", ld, k, V, z2[i:], k, top_p=p[i:], n_kept=n2[i:], row0=i, **a)
+        dd.logits_truncate(x[i:], "bf16", ld, k, V, out2[i:], top_p=p[i:])
+    assert torch.equal(z, z2) and torch.equal(n, n2) and torch.equal(out, out2)
+
+
 def test_rows_past_32_bits():
     """Row offsets beyond 2^31 numbers."""
     torch = torch_or_skip()
@@ -298,7 +315,8 @@ def test_sizes_at_which_another_kernel_begins(V, dtype):
                             dict(OFF, min_p=0.001), dict(OFF)], words_of(rng, R), sure=0.6)
 
 
-@pytest.mark.parametrize("V,dtype", [(1500, "bf16"), (50257, "bf16"), (55000, "bf16"), (140000, "bf16"), (3000, "fp32"), (20000, "fp32")])
+@pytest.mark.parametrize("V,dtype", [(1500, "bf16"), (5000, "bf16"), (12000, "bf16"), (30000, "bf16"), (50257, "bf16"), (55000, "bf16"), (140000, "bf16"),
+                                     (3000, "fp32"), (9000, "fp32"), (20000, "fp32")])
 def test_many_rows_equal_few(V, dtype):
     """A call of more rows than CUs equals calls of some of them, bit for bit: sums do not depend on the kernel."""
     torch = torch_or_skip()
