@@ -711,8 +711,9 @@ dd_status dd_token_sample(const void* logits, int32_t logits_dtype, int64_t ld, 
 
 /*
  * dd_logits_truncate - the same choice as an edit: out = l / temperature (l where that is 0) for the classes that stay, in
- * fp32, held within the type's finite numbers and rounded once, -inf for the others.  dd_posterior_sample and dd_spec_verify then draw from the
- * distribution that dd_token_sample draws from (truncate p and q alike, and the verified tokens follow the truncated target).
+ * fp32 (to the nearest; quotients below 2^-100 within a step), held within the type's finite numbers and rounded once, -inf for
+ * the others; a zero may lose its sign.  dd_posterior_sample and dd_spec_verify then draw from the distribution that
+ * dd_token_sample draws from (truncate p and q alike, and the verified tokens follow the truncated target).
  *   out          device [rows][ld]; may be logits itself, or must not overlap it; columns >= V are left untouched
  *   Row m takes the settings of entry m / rows_per_seq.  A row that allows no choice (dd_token_sample) goes through as it is.
  * Other arguments and errors as dd_token_sample.
@@ -744,8 +745,8 @@ dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t l
  *   ws           >= dd_cache_fork_workspace_bytes, 256-byte aligned; shared by no two calls that can overlap
  *   dev_err      NULL or device int32 error word
  * The call does all of this or, where something does not fit, nothing: then DD_DEVERR_CACHE is set, the new sequences hold
- * nothing (held and kv_len 0), n_free_out takes *n_free and n_moves 0; the old ones stay as they are.  That is so where the pool has too few
- * blocks, a row would pass to->ld_table entries, or an input is no fork's (a length, count, sequence or block number out
+ * nothing (held and kv_len 0), n_free_out takes *n_free and n_moves 0; the old ones stay as they are.  That is so where the
+ * pool has too few blocks, a row would pass to->ld_table entries, or an input is no fork's (a length, count, sequence or block number out
  * of range).  A block number outside [0, n_blocks) in the stack sets DD_DEVERR_CACHE.
  * While sequences share blocks, they end by dd_cache_fork (src -1 or not chosen), not by dd_cache_plan's n_new = -1, which
  * would give a shared block back under the others; and a sequence that goes back behind its `keep` tokens does so by
@@ -765,8 +766,8 @@ dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd
  *   free_blocks  [n_blocks] is written anew: n_blocks - n entries, the lowest number on top; n_free_out [1] their number
  *   moves        [n_blocks / 2][2]: (old number, new number), ascending, for dd_cache_copy; n_moves [1] their number
  *   ws           >= dd_cache_compact_workspace_bytes, 256-byte aligned; shared by no two calls that can overlap
- * Where a count or a block number of the tables is out of range, DD_DEVERR_CACHE is set, the held entries are passed on as they are, n_moves
- * is 0, and free_blocks and n_free_out are left as they were.
+ * Where a count or a block number of the tables is out of range, DD_DEVERR_CACHE is set, the held entries are passed on as they are,
+ * n_moves is 0, and free_blocks and n_free_out are left as they were.
  */
 size_t dd_cache_compact_workspace_bytes(const dd_cache* cache);
 dd_status dd_cache_compact(const dd_cache* cache, const dd_cache_map* map, int32_t* block_table_out, int32_t* free_blocks,

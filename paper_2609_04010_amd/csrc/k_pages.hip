@@ -19,6 +19,7 @@ constexpr int RW = RB / 32;         // words of its bits
 constexpr int MT = 1024;            // threads of the launches that look at ranges
 constexpr int AT = 256;             // threads of the others
 static_assert(RW == AT, "a thread per word of a range");
+constexpr int FREE_WORD = 63;       // of the first 64 words of a fork's workspace: the stack's height before it
 constexpr int SOURCES = 8192;       // old rows up to which LDS holds how much of them stays
 
 // f(block, j, head) for entry j < head.len of the rows part, part + parts, .. (block -1 behind that: no branch per lane); head(row)
@@ -231,7 +232,10 @@ DD_DEV void fork_join(const ForkArgs& a, ForkLds& sm, int range) {
     if (tid < RW && word < words) a.freed[word] = w;
     const int n = block_sum<MT>(__popc(w), sm.red);
     if (tid == 0) a.counts[range] = n;
-    if (range == 0 && tid == 0) a.bad[0] = bad;
+    if (range == 0 && tid == 0) {
+        a.bad[0] = bad;
+        a.bad[FREE_WORD] = *a.n_free;    // (the next launch may write n_free_out in its place)
+    }
 }
 
 // the r-th freed block in ascending order, by a wavefront
@@ -266,7 +270,7 @@ DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
     constexpr int W = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int s0 = wg * W;                         // sequences of this workgroup, one per wavefront
-    const int32_t n_free = *a.n_free;
+    const int32_t n_free = a.bad[FREE_WORD];
     const int bad = a.bad[0];
     int before = 0, all = 0, freed = 0;
     for (int s = tid; s < a.S_to; s += NT) {

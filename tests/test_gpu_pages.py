@@ -41,8 +41,9 @@ class Pages:
         self.n_out, self.n_moves, self.err = dev_i32(torch, [-9]), dev_i32(torch, [-9]), dev_i32(torch, [0])
         self.moves = dev_i32(torch, np.full((S_to, 2), -9))
 
-    def fork(self, c, src, keep, ws=None):
+    def fork(self, c, src, keep, ws=None, n_free=None):
         torch, cc, to = self.torch, self.cc, self.to
+        n_in = dev_i32(torch, [c[4]]) if n_free is None else n_free
         table, held, lens, free, n_free = c
         S = len(held)
         m = dd.CacheMap.empty(S, 1, table.shape[1])
@@ -50,7 +51,7 @@ class Pages:
         m.held.copy_(dev_i32(torch, held))
         self.free = dev_i32(torch, free)
         ws = torch.full((dd.cache_fork_workspace_bytes(cc, S, to.S),), 255, dtype=torch.uint8, device="cuda") if ws is None else ws
-        dd.cache_fork(cc, m, to, dev_i32(torch, lens), dev_i32(torch, src), self.free, dev_i32(torch, [n_free]), self.n_out, self.moves,
+        dd.cache_fork(cc, m, to, dev_i32(torch, lens), dev_i32(torch, src), self.free, n_in, self.n_out, self.moves,
                       self.n_moves, ws, keep=None if keep is None else dev_i32(torch, keep), dev_err=self.err)
         assert np.array_equal(m.block_table.cpu().numpy(), table) and np.array_equal(m.held.cpu().numpy(), held)
 
@@ -131,6 +132,21 @@ def test_forks_that_do_not_fit(bad):
     assert w["err"] and int(p.err.item()) == dd.DD_DEVERR_CACHE
     assert p.to.held.tolist() == [0] * 6 and p.to.kv_len.tolist() == [0] * 6 and int(p.n_moves.item()) == 0
     assert int(p.n_out.item()) == n_free and p.free.tolist() == free.tolist()
+
+
+@pytest.mark.parametrize("S", [16, 300, 20000])
+def test_the_stack_and_its_height_in_place(S):
+    """n_free_out may be n_free: workgroups that begin late still see the height before the call."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(S)
+    nb, P, ld = 3 * S, 32, 2
+    c = pool(rng, S, nb, P, ld)
+    src = rng.integers(0, S, S)
+    w = so.fork(nb, P, c[0], c[1], c[2], src, None, c[3], c[4], ld)
+    p = Pages(torch, dd.cache_config(nb, P, 1, 32), S, ld)
+    p.n_out.fill_(c[4])
+    p.fork(c, src, None, n_free=p.n_out)
+    p.same(w, c)
 
 
 def test_a_stack_with_a_wrong_number():
