@@ -25,8 +25,8 @@ constexpr int SOURCES = 8192;       // old rows up to which LDS holds how much o
 // f(block, j, head) for entry j < head.len of the rows part, part + parts, .. (block -1 behind that: no branch per lane); head(row)
 // says how long a row is, and what else f wants to know.  A wavefront takes whole rows: the heads of 64 at once, then 256
 // entries at a time.  Short code on purpose: each wavefront passes here a few times only, and fetching the instructions is
-// most of that (32 rows on their way together, unrolled, took 17 us for 1024 rows of 128 in 8 parts;
-// this takes 7, in 16).
+// most of that (32 rows on their way together, unrolled, took 17 us for 1024 rows of 128 and 25
+// ranges in 8 parts; this takes 7, in 10).
 struct Head {
     int len, whole;
 };
@@ -123,7 +123,7 @@ DD_DEV int nth_bit(uint32_t w, int r) {
 // row holds it and no new one.  owner[b]: -1 where a new row holds b whole, else the first sequence whose partly filled last
 // block it is; the other sequences of that kind take a fresh block, and a move for its contents.  What is held whole of an old row
 // is a beginning of it, the longest that any new row asks for: the new rows are not walked.  1024
-// rows of 65 entries, 10 ranges: 6 us with 25 parts, 12 with 8, 19 with one.
+// rows of 65 entries, 9 ranges: 6 us with 28 parts, 12 with 8, 19 with one.
 struct ForkLds {
     int32_t owner[RB];
     uint32_t old[RW], whole[RW], last[RW];      // held by an old row; whole by a new one; as a new one's partly filled last
