@@ -19,6 +19,7 @@ constexpr int RW = RB / 32;         // words of its bits
 constexpr int MT = 1024;            // threads of the launches that look at ranges
 constexpr int AT = 256;             // threads of the others
 static_assert(RW == AT, "a thread per word of a range");
+constexpr int ONE_LAUNCH = 128;     // sequences up to which one workgroup does everything for a pool of one range
 constexpr int FREE_WORD = 63;       // of the first 64 words of a fork's workspace: the stack's height before it
 constexpr int SOURCES = 8192;       // old rows up to which LDS holds how much of them stays
 
@@ -126,12 +127,14 @@ DD_DEV int nth_bit(uint32_t w, int r) {
 // rows of 65 entries, 9 ranges: 6 us with 28 parts, 12 with 8, 19 with one.
 struct ForkLds {
     int32_t owner[RB];
-    uint32_t old[RW], whole[RW], last[RW];      // held by an old row; whole by a new one; as a new one's partly filled last
+    uint32_t old[RW], whole[RW], part[RW];      // held by an old row; whole by a new one; as a new one's partly filled last
     int32_t most[SOURCES];                      // whole blocks of an old row that new rows hold
     int red[MT / 64], bad;
+    // in one launch, read once: where new rows come from, their last blocks, and what the phases hand on
+    int32_t src[ONE_LAUNCH], len[ONE_LAUNCH], keep[ONE_LAUNCH], last[ONE_LAUNCH], copies[ONE_LAUNCH];
 };
 
-DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
+template <bool ONE> DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
     const int tid = threadIdx.x, b0 = range * RB;
     const bool first = range == 0, fits = a.S <= SOURCES;
     for (int i = tid; i < (fits ? a.S : 0); i += MT) sm.most[i] = 0;
@@ -144,6 +147,12 @@ DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
         bad |= !fork_head(a, s, src, len, keep);
         const int n = keep >> a.c.log2p;
         if (fits && n > 0) atomicMax(&sm.most[src], n);
+        if constexpr (ONE) {
+            sm.src[s] = src;
+            sm.len[s] = len;
+            sm.keep[s] = keep;
+            sm.last[s] = keep & (a.c.P - 1) ? a.table[(int64_t)src * a.ld_table + len - 1] : -1;
+        }
     }
     __syncthreads();
     walk<MT>(a.table, a.ld_table, a.S, part, a.parts,
@@ -176,6 +185,7 @@ DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
     }
     if (bad) sm.bad = 1;
     __syncthreads();
+    if constexpr (ONE) return;
     const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
     if (tid < RW && word < words) {
         a.old[part * words + word] = sm.old[tid];
@@ -185,54 +195,56 @@ DD_DEV void fork_mark(const ForkArgs& a, ForkLds& sm, int range, int part) {
 }
 
 // the parts together: which blocks of the range are freed, and which sequences take a fresh block for one of it
-DD_DEV void fork_join(const ForkArgs& a, ForkLds& sm, int range) {
+template <bool ONE> DD_DEV void fork_join(const ForkArgs& a, ForkLds& sm, int range) {
     const int tid = threadIdx.x, b0 = range * RB;
     const int64_t word = (int64_t)range * RW + tid, words = ((int64_t)a.c.n_blocks + 31) / 32;
     for (int i = tid; i < RB; i += MT) sm.owner[i] = INT32_MAX;
     if (tid < RW) {
-        uint32_t old = 0, whole = 0;
+        if constexpr (!ONE) {
+            uint32_t old = 0, whole = 0;
 #pragma unroll 8
-        for (int k = 0; k < a.parts; ++k) {
-            old |= word < words ? a.old[k * words + word] : 0;
-            whole |= word < words ? a.whole[k * words + word] : 0;
+            for (int k = 0; k < a.parts; ++k) {
+                old |= word < words ? a.old[k * words + word] : 0;
+                whole |= word < words ? a.whole[k * words + word] : 0;
+            }
+            sm.old[tid] = old;
+            sm.whole[tid] = whole;
         }
-        sm.old[tid] = old;
-        sm.whole[tid] = whole;
-        sm.last[tid] = 0;
+        sm.part[tid] = 0;
     }
-    const bool bad = __syncthreads_or(tid < a.parts && a.bad[tid]);
-    int mine = -1;                       // this thread's first sequence's partly filled last block
-    for (int s = tid; s < a.S_to; s += MT) {
+    const bool bad = ONE ? (__syncthreads(), false) : __syncthreads_or(tid < a.parts && a.bad[tid]);
+    // the partly filled last block of a sequence, -1 without
+    auto last_block = [&](int s) -> int {
+        if constexpr (ONE) return sm.last[s];
         int src, len, keep;
         fork_head(a, s, src, len, keep);
-        if (!(keep & (a.c.P - 1))) {
-            if (range == 0) a.copies[s] = 0;
-            continue;
-        }
-        const int b = a.table[(int64_t)src * a.ld_table + len - 1];
+        return keep & (a.c.P - 1) ? a.table[(int64_t)src * a.ld_table + len - 1] : -1;
+    };
+    auto set = [&](int s, int copy) {
+        if constexpr (ONE) sm.copies[s] = copy;
+        else a.copies[s] = copy;
+    };
+    int mine = -1;                       // this thread's first sequence's
+    for (int s = tid; s < a.S_to; s += MT) {
+        const int b = last_block(s);
         const uint32_t x = (uint32_t)b - (uint32_t)b0;
-        if (range == 0 && (uint32_t)b >= (uint32_t)a.c.n_blocks) a.copies[s] = 0;
-        if (x >= RB) continue;
+        if (range == 0 && (uint32_t)b >= (uint32_t)a.c.n_blocks) set(s, 0);
         if (s == tid) mine = b;
+        if (x >= RB || b >= a.c.n_blocks) continue;
         atomicMin(&sm.owner[x], s);
-        atomicOr(&sm.last[x >> 5], 1u << (x & 31));
+        atomicOr(&sm.part[x >> 5], 1u << (x & 31));
     }
     __syncthreads();
     for (int s = tid; s < a.S_to; s += MT) {
-        int b = mine;
-        if (s != tid) {
-            int src, len, keep;
-            fork_head(a, s, src, len, keep);
-            b = keep & (a.c.P - 1) ? a.table[(int64_t)src * a.ld_table + len - 1] : -1;
-        }
+        const int b = s == tid ? mine : last_block(s);
         const uint32_t x = (uint32_t)b - (uint32_t)b0;
-        if (x < RB && b < a.c.n_blocks) a.copies[s] = (sm.whole[x >> 5] >> (x & 31) & 1) || sm.owner[x] != s;
+        if (x < RB && b < a.c.n_blocks) set(s, (sm.whole[x >> 5] >> (x & 31) & 1) || sm.owner[x] != s);
     }
-    uint32_t w = tid < RW ? sm.old[tid] & ~sm.whole[tid] & ~sm.last[tid] : 0;
+    uint32_t w = tid < RW ? sm.old[tid] & ~sm.whole[tid] & ~sm.part[tid] : 0;
     if (tid < RW && word < words) a.freed[word] = w;
     const int n = block_sum<MT>(__popc(w), sm.red);
     if (tid == 0) a.counts[range] = n;
-    if (range == 0 && tid == 0) {
+    if (!ONE && range == 0 && tid == 0) {
         a.bad[0] = bad;
         a.bad[FREE_WORD] = *a.n_free;    // (the next launch may write n_free_out in its place)
     }
@@ -265,16 +277,20 @@ DD_DEV int nth_freed(const ForkArgs& a, int r) {
 }
 
 // NT threads; workgroup wg of `wgs`
-template <int NT>
-DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
+template <int NT, bool ONE>
+DD_DEV void fork_apply(const ForkArgs& a, ForkLds* sm, int* red, int wg, int wgs) {
     constexpr int W = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int s0 = wg * W;                         // sequences of this workgroup, one per wavefront
-    const int32_t n_free = a.bad[FREE_WORD];
-    const int bad = a.bad[0];
+    const int32_t n_free = ONE ? *a.n_free : a.bad[FREE_WORD];
+    const int bad = ONE ? sm->bad : a.bad[0];
+    auto copies = [&](int s) -> int {
+        if constexpr (ONE) return sm->copies[s];
+        else return a.copies[s];
+    };
     int before = 0, all = 0, freed = 0;
     for (int s = tid; s < a.S_to; s += NT) {
-        const int c = a.copies[s];
+        const int c = copies(s);
         all += c;
         before += s < s0 ? c : 0;
     }
@@ -293,18 +309,26 @@ DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
         const int s = s1 + wv;
         if (s < a.S_to) {
             int src = 0, len = 0, keep = 0;
-            if (ok) fork_head(a, s, src, len, keep);
+            if (ok) {
+                if constexpr (ONE) {
+                    src = sm->src[s];
+                    len = sm->len[s];
+                    keep = sm->keep[s];
+                } else {
+                    fork_head(a, s, src, len, keep);
+                }
+            }
             if (lane == 0) {
                 a.to_held[s] = len;
                 a.to_len[s] = keep;
             }
             const int32_t* from = a.table + (int64_t)src * a.ld_table;
             int32_t* to = a.to_table + (int64_t)s * a.ld_to;
-            const bool copy = ok && a.copies[s];
+            const bool copy = ok && copies(s);
             for (int j = lane; j < len - copy; j += 64) to[j] = from[j];
             if (copy) {
                 int rank = before;
-                for (int i = s1; i < s; ++i) rank += a.copies[i];
+                for (int i = s1; i < s; ++i) rank += copies(i);
                 // the top of the stack once the freed blocks are on it
                 const int at = n_free + freed - 1 - rank;
                 const int b = at < n_free ? a.free_blocks[at] : nth_freed(a, at - n_free);
@@ -318,7 +342,7 @@ DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
         }
         if (s1 + wgs * W < a.S_to) {
             int c = 0;
-            for (int i = s1 + tid; i < min(s1 + wgs * W, a.S_to); i += NT) c += a.copies[i];
+            for (int i = s1 + tid; i < min(s1 + wgs * W, a.S_to); i += NT) c += copies(i);
             before += block_sum<NT>(c, red);
         }
     }
@@ -339,26 +363,25 @@ DD_DEV void fork_apply(const ForkArgs& a, int* red, int wg, int wgs) {
 
 __global__ __launch_bounds__(MT) void fork_mark_kernel(ForkArgs a) {
     __shared__ ForkLds sm;
-    fork_mark(a, sm, blockIdx.x, blockIdx.y);
+    fork_mark<false>(a, sm, blockIdx.x, blockIdx.y);
 }
 __global__ __launch_bounds__(MT) void fork_join_kernel(ForkArgs a) {
     __shared__ ForkLds sm;
-    fork_join(a, sm, blockIdx.x);
+    fork_join<false>(a, sm, blockIdx.x);
 }
 __global__ __launch_bounds__(AT) void fork_apply_kernel(ForkArgs a) {
     __shared__ int red[AT / 64];
-    fork_apply<AT>(a, red, blockIdx.x, gridDim.x);
+    fork_apply<AT, false>(a, nullptr, red, blockIdx.x, gridDim.x);
 }
-// all of it for a pool of one range and few sequences: one launch
+// all of it for a pool of one range and few sequences, in one launch that hands on in LDS (through memory: 11 us and not 8.5 for
+// one prompt to 16 continuations)
 __global__ __launch_bounds__(MT) void fork_kernel(ForkArgs a) {
     __shared__ ForkLds sm;
-    fork_mark(a, sm, 0, 0);
+    fork_mark<true>(a, sm, 0, 0);
+    fork_join<true>(a, sm, 0);
     __threadfence_block();
     __syncthreads();
-    fork_join(a, sm, 0);
-    __threadfence_block();
-    __syncthreads();
-    fork_apply<MT>(a, sm.red, 0, 1);
+    fork_apply<MT, true>(a, &sm, sm.red, 0, 1);
 }
 
 // ---------------------------------------------------------------- compaction
@@ -543,9 +566,8 @@ __global__ __launch_bounds__(CT) void copy_kernel(CopyArgs a) {
 
 }  // namespace
 
-// Sequences up to which one workgroup does everything for a pool of one range (16 sequences compact in 7 us, and took 9 in three
-// launches); sequences of a part, two for a wavefront.
-constexpr int ONE_LAUNCH = 128, PER_PART = 2 * MT / 64;
+// ONE_LAUNCH: 16 sequences compact in 7 us, and took 9 in three launches.  Sequences of a part: two for a wavefront.
+constexpr int PER_PART = 2 * MT / 64;
 
 static int parts_for(int ranges, int32_t S) { return std::max(1, std::min(page_parts(ranges), S / PER_PART)); }
 
