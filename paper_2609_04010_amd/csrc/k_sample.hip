@@ -816,6 +816,7 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
         auto each_chunk = [&](auto&& f) {
             constexpr int AHEAD = 4;       // chunks whose loads are under way together
             for (int c0 = 0; c0 < chunks; c0 += AHEAD) {
+                const bool whole = (c0 + AHEAD) * NT * E <= a.V;
                 uint4 u[AHEAD];
 #pragma unroll
                 for (int c = 0; c < AHEAD; ++c)      // (no branch between the loads; ld is a multiple of 8: in bounds)
@@ -824,8 +825,10 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
                 for (int c = 0; c < AHEAD; ++c) {
                     const int v = ((c0 + c) * NT + tid) * E;
                     if (c0 + c >= chunks) break;
-                    if (v >= a.V) u[c] = Elem<T>::NEG_INF4;
-                    else if (v + E > a.V) Elem<T>::clip(u[c], a.V - v);
+                    if (!whole) {
+                        if (v >= a.V) u[c] = Elem<T>::NEG_INF4;
+                        else if (v + E > a.V) Elem<T>::clip(u[c], a.V - v);
+                    }
                     float x[E];
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[e] = Elem<T>::get(u[c], e);
