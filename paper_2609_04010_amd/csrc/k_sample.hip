@@ -98,7 +98,8 @@ DD_DEV bool quotient_fits(float t, float a, float b) {
 // the window spans 16 binades).  Where a bound falls among those, or among numbers below the window (top-k alone can ask for
 // them), the next window is counted.  Two packed numbers are handled at a time, and the row stays in registers.
 //
-// Rows of 50257 classes under temperature, top-k and top-p: 8 in 16 us, 512 in 30; 4096 truncated in 174 (4.7 TB/s read and
+// Rows of 50257 classes under temperature, top-k and top-p: 8 in 16 us, 512 in 31 (of a row's 24 there, two on a CU: 7 for the
+// loads, 3 for the largest, 7 for counting, 2.5 each for the sums and the search, 1.2 for the class); 4096 truncated in 174 (4.7 TB/s read and
 // written; with a division per number and its edges tested one by one 560).
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
@@ -735,10 +736,10 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
 // ---------------------------------------------------------------- fp32 rows, and bf16 rows of very many classes
 //
 // Every pass reads the row again, from L2 after the first.  (With the row in registers, 52 of them, the compiler keeps
-// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 65.)  Bins are steps of the exponential's
+// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 63.)  Bins are steps of the exponential's
 // table, so a number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
 // of the bin where a bound lies are listed with their weights, and each sums those before it.  Draws that follow each
-// other from one row under the same settings share all but the last step.  333 truncated rows of 32003 take 55 us.
+// other from one row under the same settings share all but the last step.  333 truncated rows of 32003 take 51 us.
 template <int NT>
 struct StreamLds {
     static constexpr int NW = NT / 64;
