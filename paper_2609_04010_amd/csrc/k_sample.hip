@@ -739,7 +739,8 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
 // the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 63.)  Bins are steps of the exponential's
 // table, so a number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
 // of the bin where a bound lies are listed with their weights, and each sums those before it.  Draws that follow each
-// other from one row under the same settings share all but the last step.  333 truncated rows of 32003 take 51 us.
+// other from one row under the same settings share all but the last step.  A truncated row is
+// written while its last bin is listed, unless that is in place: 333 rows of 32003 take 48 us, and 51 with a pass of its own.
 template <int NT>
 struct StreamLds {
     static constexpr int NW = NT / 64;
@@ -991,6 +992,48 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
             }
             continue;
         }
+        // a chunk of the truncated row: f(number, class) says what stays
+        const bool divide = t != 1.f && t != 0.f;
+        const float rt = 1.f / t;
+        constexpr float largest = sizeof(T) == 2 ? 0x1.FEp127f : FLT_MAX;   // (quotients do not become infinite)
+        float edge = state == 2 ? q.least : q.top;   // nothing below it stays
+        bool written = false;
+        uint32_t stay_n = 0;
+        auto over_t = [&](float x) {
+            return quotient_fits(t, q.top, edge) ? quotient(x, t, rt) : fminf(fmaxf(x / t, -largest), largest);
+        };
+        auto put = [&](const float (&x)[E], int v, auto&& f) {
+            T* out = (T*)a.out + (int64_t)r * a.ld;
+            if (v >= a.V) return;
+            float y[E];
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = f(x[e], v + e);
+                stay_n += in;
+                any |= in;
+                y[e] = in ? x[e] : -INFINITY;
+            }
+            if (divide && any)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float z = over_t(x[e]);
+                    y[e] = y[e] == -INFINITY ? y[e] : z;
+                }
+            if (v + E <= a.V) {
+                if constexpr (sizeof(T) == 2)
+                    *(uint4*)(out + v) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+                else
+                    *(float4*)(out + v) = make_float4(y[0], y[1], y[2], y[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (v + e >= a.V) continue;
+                    if constexpr (sizeof(T) == 2) out[v + e] = f32_to_bf16(y[e]);
+                    else out[v + e] = y[e];
+                }
+            }
+        };
         if (state == 2 && (DRAW || step == 0)) {
             for (; step < (DRAW ? 3 : 2); ++step) {
                 bool count = false;
@@ -1035,12 +1078,17 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
                 const float from = bin1 == BINS - 1 ? -FLT_MAX : (float)fmax((double)q.top - ((double)n1 + 0.75) / q.turn, -FLT_MAX);
                 const float upto = bin1 == 0 ? q.top : (float)fmax((double)q.top - ((double)n0 - 0.75) / q.turn, -FLT_MAX);
                 const float low = fmaxf(from, q.least), high = fmaxf(upto, low);
+                edge = low;
+                // the last pass but for the bin's numbers: what is larger stays.  (Not in place: the bin may have to be read again)
+                const bool ahead = !DRAW && a.out != a.logits && (step == 1 || !(p < 1.f));
                 // (a draw's pass counts what stays, if that is asked for and top-k has not said it)
                 const bool tally = step == 2 && a.kept && !counted;
                 const float last = key_value((uint32_t)(cut >> 32));
                 uint32_t stay = 0;
                 each_chunk([&](const float (&x)[E], int v) {
                     bool in[E], any = false;
+                    if constexpr (!DRAW)
+                        if (ahead) put(x, v, [&](float x, int) { return x > high; });
                     if (tally)
 #pragma unroll
                         for (int e = 0; e < E; ++e)
@@ -1072,7 +1120,8 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
                     counted = true;
                 }
                 int n = same(sm.listed);
-                if (n <= CANDS) {
+                const bool few = n <= CANDS;
+                if (few) {
                     if (tid < n) {
                         int bin;
                         const uint64_t w = weight_of(sm.value[tid], bin);
@@ -1171,6 +1220,18 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
                 }
                 __syncthreads();
                 at = same(sm.at);
+                if (!DRAW && ahead) {
+                    written = few;
+                    if (!few) {
+                        stay_n = 0;
+                    } else if (tid < n && place(sm.value[tid], sm.id[tid]) <= at) {
+                        const float y = divide ? over_t(sm.value[tid]) : sm.value[tid];
+                        T* out = (T*)a.out + (int64_t)r * a.ld + sm.id[tid];
+                        if constexpr (sizeof(T) == 2) *out = f32_to_bf16(y);
+                        else *out = y;
+                        ++stay_n;
+                    }
+                }
                 if (step < 2) {
                     cut = at;
                     kept_w = same(sm.before_w);
@@ -1194,44 +1255,9 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
             }
         }
         if constexpr (!DRAW) {
-            T* out = (T*)a.out + (int64_t)r * a.ld;
-            constexpr float largest = sizeof(T) == 2 ? 0x1.FEp127f : FLT_MAX;   // (quotients do not become infinite)
-            const bool divide = t != 1.f && t != 0.f, fast = quotient_fits(t, q.top, all ? q.least : last);
-            const float rt = 1.f / t;
-            uint32_t n = 0;
-            each_chunk([&](const float (&x)[E], int v) {
-                if (v >= a.V) return;
-                float y[E];
-                bool any = false;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const bool in = stays(x[e], v + e);
-                    n += in;
-                    any |= in;
-                    y[e] = in ? x[e] : -INFINITY;
-                }
-                if (divide && any)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float z = fast ? quotient(x[e], t, rt) : fminf(fmaxf(x[e] / t, -largest), largest);
-                        y[e] = y[e] == -INFINITY ? y[e] : z;
-                    }
-                if (v + E <= a.V) {
-                    if constexpr (sizeof(T) == 2)
-                        *(uint4*)(out + v) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-                    else
-                        *(float4*)(out + v) = make_float4(y[0], y[1], y[2], y[3]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        if (v + e >= a.V) continue;
-                        if constexpr (sizeof(T) == 2) out[v + e] = f32_to_bf16(y[e]);
-                        else out[v + e] = y[e];
-                    }
-                }
-            });
+            if (!written) each_chunk([&](const float (&x)[E], int v) { put(x, v, stays); });
             if (a.kept) {
-                n = wave_scan(n);
+                const uint32_t n = wave_scan(stay_n);
                 if (tid == 0) sm.count = 0;
                 __syncthreads();
                 if (lane == 63) atomicAdd(&sm.count, n);
