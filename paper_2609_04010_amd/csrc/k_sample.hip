@@ -1192,7 +1192,9 @@ __global__ __launch_bounds__(NT, 4) void sample_stream_kernel(SampleArgs a) {
                         base_w = same(sm.before_w);
                         n = (int)same(sm.in_c);
                         lo = first + ((uint64_t)same(sm.bin) << shift);
-                        hi = lo + ((1ull << shift) - 1);
+                        // (no further than the range that was cut: a part's end lies past the last one's, and past 64 bits)
+                        const uint64_t width = (1ull << shift) - 1;
+                        hi = past - lo < width ? past : lo + width;
                         __syncthreads();
                     } while (n > CANDS);
                     each([&](uint64_t at, uint64_t w) {

@@ -380,3 +380,34 @@ def test_draws_of_one_row_equal_single_ones(V, dtype):
     for u, v in zip(*got):
         assert torch.equal(u, v)
     assert (got[0][0][dev_i32(torch, ids) == -1] == -9).all() and len(set(got[0][0].tolist())) > 100
+
+
+@pytest.mark.parametrize("V,R,dtype", [(985, 6, "fp32"), (3000, 600, "fp32"), (9000, 6, "fp32"), (9000, 300, "fp32"), (140000, 3, "bf16")])
+def test_a_bin_that_is_cut_again(V, R, dtype):
+    """Five values under a temperature that puts all in one bin.  The zeros before the first of the largest fall into the part
+    of the numbers just above them, which is cut again: what is listed then ends where that part ends."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    l = rng.choice([1.0, 1e-40, 0.0, -1e-40, -1.0], V)
+    l[:9], l[9] = 0.0, 1.0
+    l = np.tile(round_to_dtype(l[None], dtype), (R, 1))
+    up, t = int((l[0] > 0).sum()), f32(1e11)
+    at = np.concatenate([np.arange(up - 4, up + 14), rng.integers(1, V, R)])[:R] if R > 20 else up + np.arange(R)
+    # the at-th class in order, as all weights are next to 1; and at classes
+    words = np.floor((at + 0.5) / V * 2.0 ** 32).astype(np.uint64)
+    check(torch, l, dtype, [dict(OFF, temperature=t)] * R, words, sure=1.0)
+    check(torch, l, dtype, [dict(OFF, temperature=t, top_k=int(k)) for k in at], words, sure=0.9)
+    check(torch, l, dtype, [dict(OFF, temperature=t, top_p=float(k) / V) for k in at], words, sure=0.9)
+
+
+@pytest.mark.parametrize("R", [6, 600])
+def test_a_bin_that_reaches_the_lowest_numbers(R):
+    """Numbers that weigh nothing stand in one bin down to the type's lowest: its last part would end past 64 bits."""
+    torch = torch_or_skip()
+    V = 2100
+    rng = np.random.default_rng(5)
+    l = np.sign(rng.normal(size=V)) * 10.0 ** rng.uniform(-40, 37, V)
+    l[rng.permutation(V)[:100]] = -2.0 ** 127 * rng.uniform(1, 1.99, 100)
+    l = np.tile(round_to_dtype(l[None], "fp32"), (R, 1))
+    k = V - np.array([1, 2, 30, 60, 95, 100]) if R == 6 else V - np.arange(R) // 3
+    check(torch, l, "fp32", [dict(OFF, top_k=int(x)) for x in k], words_of(rng, R), sure=1.0)
