@@ -728,7 +728,8 @@ dd_status dd_logits_truncate(const void* logits, int32_t logits_dtype, int64_t l
  * dd_cache_fork - the sequences of the next passes from those that there are: each takes the first tokens of some sequence's
  * context (several continuations of a prompt, candidates chosen anew, requests that end).  Whole blocks are shared, no
  * key or value is copied here; a partly filled last block belongs to one sequence alone, since that appends into it.
- *   map          the old sequences: S, ld_table, block_table, held, kv_len (its row arrays are not looked at); S <= 2^16
+ *   map          the old sequences: S, ld_table, block_table, held, kv_len (lengths are read from seq_len; the row arrays are not
+ *                looked at); S <= 2^16
  *   to           the new ones, S and ld_table of their own; block_table, held and kv_len are written and overlap no array of
  *                the old ones.  Entries beyond a sequence's own are left as they were.
  *   seq_len      [map->S] tokens that each old sequence has, at most held * P (map->kv_len after a pass)
@@ -761,7 +762,8 @@ dd_status dd_cache_fork(const dd_cache* cache, const dd_cache_map* map, const dd
 /*
  * dd_cache_compact - the blocks in use to the lowest numbers of the pool, so that it can shrink.  With n blocks in use, the i-th
  * of them that is n or more moves to the i-th number below n that is not in use.
- *   map          S, ld_table, block_table and held are read; S <= 2^16
+ *   map          S, ld_table, block_table and held are read; kv_len is not, but may not be NULL where S > 0 (a map is complete in
+ *                every call); S <= 2^16
  *   block_table_out  [S][ld_table], may be map->block_table: the tables under the new numbers, held entries alone
  *   free_blocks  [n_blocks] is written anew: n_blocks - n entries, the lowest number on top; n_free_out [1] their number
  *   moves        [n_blocks / 2][2]: (old number, new number), ascending, for dd_cache_copy; n_moves [1] their number
