@@ -533,8 +533,8 @@ __global__ __launch_bounds__(MT) void compact_kernel(CompactArgs a) {
 //
 // A block's codes of all heads stand one behind the other, H 2 P dh bytes, and so do its scales.  A workgroup copies a piece of
 // one block in one layer, 16 bytes per thread, and takes another while there are any: how many moves there are, only the
-// device knows.  Bound by the memory: 4.9 TB/s read and written at 1024 moves of 98304 bytes in 12 layers, 492 us; 16 of them
-// take 7.7.  One load per thread and many short workgroups: two or four loads per thread cost the small copy 9 us, and the large
+// device knows.  Bound by the memory: 4.9 TB/s read and written at 1024 moves of 98304 bytes in 12 layers, 494 us; 16 of them
+// take 7.7 on the same 38 MB again and again, which the last-level cache keeps, and 11.5 on those of 12 pools in turn.  One load per thread and many short workgroups: two or four loads per thread cost the small copy 9 us, and the large
 // one 5.  16 workgroups per CU and not as many as there are pieces: 484 us at 64 per CU, but an empty list would pay for those.
 constexpr int CT = 512;
 constexpr int PIECE = CT * 16;
@@ -583,6 +583,8 @@ dd_status launch_cache_fork(const ForkArgs& args, hipStream_t s) {
         return launch_status("cache_fork");
     }
     a.parts = parts_for(a.ranges, a.S);
+    // (The last launch has a wavefront per new sequence; each workgroup sums the copies of all, and together they push the freed
+    // blocks of all ranges.  Both show at the ends: 1024 sequences of 512 tokens into 65536 take 513 us, 16384 of 4096 into 4 take 994.)
     go(fork_mark_kernel, dim3((unsigned)a.ranges, (unsigned)a.parts), MT);
     go(fork_join_kernel, dim3((unsigned)a.ranges), MT);
     go(fork_apply_kernel, dim3((unsigned)std::max<int64_t>(1, ceil_div(a.S_to, AT / 64))), AT);

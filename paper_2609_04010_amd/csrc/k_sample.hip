@@ -95,12 +95,13 @@ DD_DEV bool quotient_fits(float t, float a, float b) {
 // numbers are all that a bin holds, so a count gives its weight, the exponential is taken once per bin, and a bound
 // inside a bin is a division away.  A window of keys stands in LDS: MAGS magnitudes of either sign below the largest that can
 // matter (weights below e^-34 round to 0), with the numbers nearer to 0 in one bin between them, whose weights are summed one by one (few:
-// the window spans 16 binades).  Where a bound falls among those, or among numbers below the window (top-k alone can ask for
-// them), the next window is counted.  Two packed numbers are handled at a time, and the row stays in registers.
+// the window spans 16 binades, 32 in 512 threads and more).  Where a bound falls among those, or among numbers below the window (top-k
+// alone can ask for them), the next window is counted.  Two packed numbers are handled at a time, and the row stays in registers; at
+// their limit of 128, draws spill 2 registers with 8 chunks per thread, 5 with 13 and up to 19 with 16.
 //
-// Rows of 50257 classes under temperature, top-k and top-p: 8 in 16 us, 512 in 31 (of a row's 24 there, two on a CU: 7 for the
-// loads, 3 for the largest, 7 for counting, 2.5 each for the sums and the search, 1.2 for the class); 4096 truncated in 174 (4.7 TB/s read and
-// written; with a division per number and its edges tested one by one 560).
+// Rows of 50257 classes under temperature, top-k and top-p: 8 in 16 to 19 us, 512 in 31 to 34 (of a row's 24 there, two on a CU: 7 for the
+// loads, 3 for the largest, 7 for counting, 2.5 each for the sums and the search, 1.2 for the class); 4096 truncated in 175 (4.7 TB/s read and
+// written; 284 with a division per number, all numbers counted, and rows written number by number).
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
                 for (;;) {
                     if (!have) {                       // the main window is the one that stands
                         if (step == 0) {
-                            const bool further = kn < -win.max && kmin < -win.max;      // numbers below the window
+                            const bool further = kn < -win.max && kmin < -win.max;      // numbers below the window, or -inf
                             if (k > 0 && (uint32_t)k < kept_c) {
                                 count = have = true;
                                 bound = (uint32_t)k;
@@ -563,7 +564,8 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
             }
             __syncthreads();
             if (same(sm.ask)) {
-                // numbers below the window
+                // numbers below the window.  (Where only -inf stands there, also behind the last class, the window is counted again
+                // for nothing: 512 draws under temperature alone take 39.8 us with n_kept, and 26.7 without)
                 uint32_t x = 0;
 #pragma unroll
                 for (int y = 0; y < CH * 4; ++y)
@@ -736,9 +738,11 @@ __global__ __launch_bounds__(NT, 4) void sample_keys_kernel(SampleArgs a) {
 // ---------------------------------------------------------------- fp32 rows, and bf16 rows of very many classes
 //
 // Every pass reads the row again, from L2 after the first.  (With the row in registers, 52 of them, the compiler keeps
-// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 63.)  Bins are steps of the exponential's
+// the rest in scratch memory: 512 draws from 16 rows of 50257 took 81 us, and take 54 to 66 with the rows' values.)  Bins are steps of the exponential's
 // table, so a number's bin falls out of its weight; numbers that weigh nothing share the last one.  A bin holds different numbers: those
-// of the bin where a bound lies are listed with their weights, and each sums those before it.  Draws that follow each
+// of the bin where a bound lies are listed with their weights, and each sums those before it; where they are too many for that, their
+// places are cut into parts first, with three readings of the row number by number (512 draws of 50257 classes: 354 us at a temperature that
+// puts all in one bin, 65 at 1).  Draws that follow each
 // other from one row under the same settings share all but the last step.  A truncated row is
 // written while its last bin is listed, unless that is in place: 333 rows of 32003 take 48 us, and 51 with a pass of its own.
 template <int NT>
@@ -1279,7 +1283,8 @@ static void launch_sample_keys(const SampleArgs& a, hipStream_t s) {
     // few each (a wavefront's share of the search is the same for any).  At up to a CU, up to two and more rows per CU, draws
     // under top-p: 32000 classes, 200 rows 14.0 us in 1024 threads and 15.1 in 512, 300 rows 24.1 and 19.7; 8000 classes, 500 rows 13.8
     // in 512 and 14.7 in 256, 700 rows 19.8 and 17.0; 16000 classes, 500 rows 16.2 and 17.7, 1024 rows 28.4 and 24.4;
-    // 50257 classes, 200 rows 17.9 in 1024 and 18.7 in 512, 300 rows 31.6 and 24.7.
+    // 50257 classes, 200 rows 17.9 in 1024 and 18.7 in 512, 300 rows 31.6 and 24.7.  Between 32769 and 53248 classes a row pays for
+    // all chunks: 33000, 40000 and 50257 under top-k too, 200 rows 22.8, 23.1 and 24.7, 300 rows 29.2, 28.5 and 31.0.
     const int cus = num_cus();
     const bool few = a.n <= cus, some = a.n <= 2 * (int64_t)cus;
     if (a.V <= 2048) go(sample_keys_kernel<256, 1, DRAW>, 256);
@@ -1301,7 +1306,8 @@ static void launch_sample_t(const SampleArgs& args, hipStream_t s) {
     if constexpr (sizeof(T) == 2) {
         if (a.V <= 131072 && grid_fits(a.n, 1024)) return launch_sample_keys<DRAW>(a, s);
     }
-    // Draws that share a row and its settings are one workgroup's as far as every CU has one.
+    // Draws that share settings, and may share a row, are one workgroup's as far as every CU has one.  (Where they do not, that
+    // costs: 4096 draws from as many rows of 32000 take 512 us with 16 draws to a setting, and 317 with one.)
     a.chunk = DRAW && a.per > 1 && a.row_ids ? (int)std::max<int64_t>(1, a.n / num_cus()) : 1;
     if (!grid_fits(ceil_div(a.n, a.chunk), 1024)) a.chunk = 1024;
     auto go = [&](auto kernel, int threads) { launch_k(kernel, dim3((unsigned)ceil_div(a.n, a.chunk)), dim3(threads), 0, s, a); };
