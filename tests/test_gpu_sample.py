@@ -411,3 +411,47 @@ def test_a_bin_that_reaches_the_lowest_numbers(R):
     l = np.tile(round_to_dtype(l[None], "fp32"), (R, 1))
     k = V - np.array([1, 2, 30, 60, 95, 100]) if R == 6 else V - np.arange(R) // 3
     check(torch, l, "fp32", [dict(OFF, top_k=int(x)) for x in k], words_of(rng, R), sure=1.0)
+
+
+@pytest.mark.parametrize("V,dtype", [(33, "fp32"), (33, "bf16"), (6000, "fp32"), (6000, "bf16")])
+def test_rows_one_call_each(V, dtype):
+    """Rows of one call equal, bit for bit, the same rows in calls of their own."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    R, ld = 600, int(dd.logits_ld(V))
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((R, ld), generator=g, device="cuda") * 4
+    x = x.bfloat16() if dtype == "bf16" else x
+    a = settings(torch, draw_settings(rng, R, V), NAMES)
+    words = dev_words(torch, words_of(rng, R))
+    got = []
+    for k in (R, 1):
+        z, n, n2, err = (dev_i32(torch, np.full(m, -9)) for m in (R, R, R, 1))
+        err.zero_()
+        logp, out = torch.zeros(R, device="cuda"), torch.full_like(x, 3.0)
+        for i in range(0, R, k):
+            s = {name: t[i:i + k] for name, t in a.items()}
+            dd.token_sample(x[i:i + k], dtype, ld, k, V, z[i:i + k], k, noise_words=words[i:i + k], logp=logp[i:i + k], n_kept=n[i:i + k], dev_err=err, **s)
+            dd.logits_truncate(x[i:i + k], dtype, ld, k, V, out[i:i + k], n_kept=n2[i:i + k], dev_err=err, **s)
+        assert int(err.item()) == 0 and torch.equal(n, n2)
+        got.append((z, n, logp, out))
+    for u, v in zip(*got):
+        assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("V", [985, 9000, 50257])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_settings_at_their_ends(V, dtype):
+    """Smallest and largest temperatures, shares next to 0 and 1, counts around a workgroup's threads."""
+    torch = torch_or_skip()
+    rng = np.random.default_rng(V)
+    under = 1 - 2.0 ** -24
+    some = [dict(temperature=t) for t in (1e-44, 1e-30, 3e38)] + [dict(top_p=p) for p in (0.0, 1e-30, under, np.inf)] + \
+        [dict(min_p=m) for m in (1e-45, 1e-10, under)] + [dict(top_k=k) for k in (1, 255, 256, 257, 511, 512, 513, 1024, 1025, V - 1, V, 2 ** 31 - 1, -2 ** 31)] + \
+        [dict(temperature=1e20, top_k=V // 2, top_p=0.5), dict(temperature=1e-3, top_k=V - 1), dict(temperature=0.01, top_k=700, top_p=under, min_p=1e-30)]
+    some = [dict(OFF, **s) for s in some]
+    R = len(some)
+    l = round_to_dtype(rng.normal(size=(R, V)) * rng.choice([0.5, 3.0, 40.0], (R, 1)), dtype)
+    l[rng.random(l.shape) < 0.1] = -np.inf
+    l[:, V // 2] = 1.0
+    check(torch, l, dtype, some, rng.integers(2 ** 28, 2 ** 32 - 2 ** 28, R, dtype=np.uint64), sure=0.9)
